@@ -100,7 +100,8 @@ typedef enum archead_op {
   ARCHEAD_OP_LOGITS_CE = 1, /* archead_logits_ce */
   ARCHEAD_OP_ARGMAX = 2,    /* archead_logits_argmax */
   ARCHEAD_OP_TOPK = 3,      /* archead_logits_topk */
-  ARCHEAD_OP_FIDELITY = 4   /* archead_logit_fidelity_head */
+  ARCHEAD_OP_FIDELITY = 4,  /* archead_logit_fidelity_head */
+  ARCHEAD_OP_BEAM = 5       /* archead_logits_beam (M = B * K rows) */
 } archead_op;
 
 /* Shape and encoding of a packed head (the "integer shapes/groups" metadata
@@ -564,6 +565,148 @@ archead_status archead_build_head(const archead_build_desc* b, const float* W, i
                                   const float* H, int64_t ldh, const double* omega,
                                   const archead_ptrs* out, double* a_w, double* b_w, void* ws,
                                   size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Products of 8-bit integers: an INT8 head with one scale per vocabulary row
+ * (the "Row INT8" head the paper compares with, Section 4) on activations
+ * rounded to 8 bits per token, or any other layer in that form.
+ *
+ * archead_quantize_i8 rounds the rows of x to 8 bits: for m < M
+ *   scales[m]   = max(max_i |x[m, i]| / 127 rounded to fp32, 2^-126),
+ *   codes[m, i] = the integer nearest to x[m, i] / scales[m] (the exact
+ *                 quotient; halves to even), in [-127, 127].
+ * A row that holds an infinity or a NaN gets scale NaN and codes 0, so that
+ * products with it are NaN.  Rows may be tokens or, for weights, channels.
+ *   x       fp32, bf16 or fp16 [M, ldx] device, aligned to its element size,
+ *           ldx >= d >= 1
+ *   codes   int8 [M, ldc] device, ldc >= d (elements past d of a row are left
+ *           as they were);  scales  device fp32 [M], 4-byte aligned
+ *   stream  hipStream_t (NULL = the default stream); asynchronous
+ * codes and scales share no memory with x.  M = 0 is a no-op.
+ * ARCHEAD_E_INVALID_ARG for a null pointer, M < 0 or M >= 2^31, d < 1 or
+ * d >= 2^31, a leading dimension < d or a dtype not listed;
+ * ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when the launch fails. */
+archead_status archead_quantize_i8(const void* x, archead_dtype x_dtype, int64_t M, int64_t d,
+                                   int64_t ldx, int8_t* codes, int64_t ldc, float* scales,
+                                   void* stream);
+
+/* out[m, n] = (sum_k a[m, k] b[n, k]) a_scales[m] b_scales[n] (+ bias[n]),
+ * m < M, n < N: the sum exact (32-bit integers), then the products with
+ * a_scales and b_scales and the bias in fp32, in this order, rounded once more
+ * (to nearest even) for bf16 and fp16 outputs.
+ *   a         int8 [M, lda] device (any alignment), lda >= K
+ *   b         int8 [N, ldb] device (any alignment), ldb >= K
+ *   a_scales  fp32 [M], b_scales fp32 [N], bias fp32 [N] or NULL, device,
+ *             4-byte aligned
+ *   out       fp32, bf16 or fp16 [M, ldo] device, aligned to its element size,
+ *             ldo >= N, sharing no memory with the inputs
+ *   stream    hipStream_t (NULL = the default stream); asynchronous
+ * a and b at 16-byte aligned addresses with K, lda and ldb multiples of 16
+ * take the faster kernels.  M = 0 or N = 0 is a no-op; with K = 0 the sums are 0.  ARCHEAD_E_INVALID_ARG for a null pointer, a negative
+ * size, M or N >= 2^31, a leading dimension too small or a dtype not listed;
+ * ARCHEAD_E_UNSUPPORTED for K > 131071 (the sum would pass 32 bits);
+ * ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when a launch fails. */
+archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const float* a_scales,
+                                 const int8_t* b, int64_t ldb, const float* b_scales,
+                                 const float* bias, int64_t M, int64_t N, int64_t K, void* out,
+                                 archead_dtype out_dtype, int64_t ldo, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Beam search: the choice of the next hypotheses, and the states they
+ * continue.  B sequences of K beams each; row b * K + k belongs to beam k of
+ * sequence b.
+ */
+#define ARCHEAD_BEAM_MAX 32   /* largest K */
+
+/* Bytes of workspace archead_beam_select needs for `rows` = B * K rows of V
+ * logits (0 for rows < 1 or V < 1). */
+size_t archead_beam_workspace_bytes(int64_t rows, int64_t V);
+
+/* The n best continuations of each sequence: with
+ *   score(k, v) = scores[b, k] + (logit[b K + k, v] - logsumexp(logit[b K + k, :]))
+ * for every beam k and token v, the n pairs (k, v) of largest score in
+ * decreasing order, equal scores by increasing k, then v.  Within a beam the
+ * order is that of the logits; between beams that of scores in fp64 from fp32
+ * exponentials summed in a fixed order.  out_scores has the score rounded to
+ * fp32.
+ *   - Only scores above -inf are candidates: tokens with logit -inf are not,
+ *     nor any token of a beam whose own score is not finite (a beam not yet
+ *     begun has -inf; its logits are not read), or whose logits hold a NaN or
+ *     +inf or nothing above -inf.
+ *   - A beam with finished[b, k] != 0 offers one candidate, (k, end_token)
+ *     with its score unchanged; its logits are not read.
+ *   - Places that fewer than n candidates leave empty get score -inf, parent
+ *     -1 and token -1.
+ *   logits       fp32, bf16 or fp16 [B * K, ldl] device, aligned to its
+ *                element size, ldl >= V
+ *   scores       device fp32 [B, K];  finished  device bytes [B, K] or NULL
+ *   end_token    the token that ends a hypothesis, in [0, V), or -1 for none
+ *                (then finished must be NULL)
+ *   n            1 <= n <= ARCHEAD_TOPK_MAX
+ *   out_scores   device fp32 [B, n];  parents, tokens  device int64 [B, n]
+ *   out_finished device bytes [B, n] or NULL: 1 where the parent had finished
+ *                or the token is end_token, else 0
+ *   ws           device scratch of archead_beam_workspace_bytes(B * K, V)
+ *                bytes, 256-byte aligned, contents on entry do not matter
+ *   stream       hipStream_t (NULL = the default stream); asynchronous
+ * With n == K, out_scores may be scores and out_finished may be finished;
+ * outputs share no other memory with inputs.  B = 0 is a no-op.  The result
+ * is reproducible.  ARCHEAD_E_INVALID_ARG for a null pointer, B < 0,
+ * K outside [1, ARCHEAD_BEAM_MAX], B * K > 65535, V < 1 or V >= 2^31, n or
+ * end_token out of range, ldl < V, finished without end_token, or a dtype
+ * not listed; ARCHEAD_E_MISALIGNED; ARCHEAD_E_WORKSPACE; ARCHEAD_E_HIP. */
+archead_status archead_beam_select(const void* logits, archead_dtype logits_dtype, int64_t B,
+                                   int64_t K, int64_t V, int64_t ldl, const float* scores,
+                                   const uint8_t* finished, int64_t end_token, int32_t n,
+                                   float* out_scores, int64_t* parents, int64_t* tokens,
+                                   uint8_t* out_finished, void* ws, size_t ws_bytes, void* stream);
+
+/* archead_beam_select over the packed head's fp32 logits of the B * K tokens x
+ * (those of archead_logits for M = B * K), which stay in the workspace:
+ * archead_workspace_bytes(h, B * K, ARCHEAD_OP_BEAM) bytes.  x and ldx as
+ * archead_logits, the rest as archead_beam_select; errors of both. */
+archead_status archead_logits_beam(const archead_handle* h, const void* x, int64_t B, int64_t K,
+                                   int64_t ldx, const float* scores, const uint8_t* finished,
+                                   int64_t end_token, int32_t n, float* out_scores,
+                                   int64_t* parents, int64_t* tokens, uint8_t* out_finished,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/* Layout of the states of one kind (say, the keys and values of every layer):
+ * a row (one beam) is n_outer blocks (say, heads) of `positions` positions of
+ * pos_bytes contiguous bytes.  All strides in bytes, of the source and of the
+ * destination. */
+typedef struct archead_state_layout {
+  int64_t n_outer, positions, pos_bytes;
+  int64_t src_row, src_outer, src_pos;
+  int64_t dst_row, dst_outer, dst_pos;
+} archead_state_layout;
+
+/* States of the chosen beams: for each state i < n_states, sequence b and
+ * j < n, row b * n + j of dst[i] becomes row b * K + parents[b, j] of src[i],
+ * in its first lengths[b] positions (all of them without lengths; lengths
+ * are clamped to [0, positions]).  Everything else of dst stays as it was:
+ * positions from lengths[b] on, and rows whose parent is outside [0, K) (the
+ * empty places of archead_beam_select).
+ *   src, dst   host arrays of n_states device pointers, read before the call
+ *              returns.  dst[i] == src[i] for every i reorders in place (then
+ *              n == K and the strides agree): any parents, cycles among
+ *              them; rows that keep their place are not touched.  Otherwise
+ *              no destination shares memory with a source.  No two
+ *              destinations share memory, nor two rows of one.
+ *   parents    device int32 or int64 [B, n] (idx_dtype ARCHEAD_I32 / I64)
+ *   lengths    device int32 [B] or NULL
+ *   stream     hipStream_t (NULL = the default stream); asynchronous
+ * Each source row is read once however many beams continue it.  Pointers,
+ * strides and pos_bytes that are multiples of 16 are fastest (of 4: less so;
+ * of 1: slow).  n_states = 0, B = 0 or empty rows are a no-op.
+ * ARCHEAD_E_INVALID_ARG for a null pointer, a negative size or stride, K
+ * outside [1, ARCHEAD_BEAM_MAX], n outside [1, ARCHEAD_TOPK_MAX], B >= 2^31 / 64, a
+ * mixture of states in place and not, in place with n != K or other strides;
+ * ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when a launch fails. */
+archead_status archead_beam_reorder(const archead_state_layout* layout, int64_t n_states,
+                                    const void* const* src, void* const* dst, int64_t B, int64_t K,
+                                    int64_t n, const void* parents, archead_dtype idx_dtype,
+                                    const int32_t* lengths, void* stream);
 
 /* Persistent bytes of the packed head: the sum over its buffers of element
  * count times element size (the paper's bytes(ARCHead), Section 3.3).

@@ -6,15 +6,19 @@ device memory and streams only.
 """
 from .archead import (  # noqa: F401
     ArcheadError,
+    BeamStates,
     BuildDesc,
     Desc,
+    beam_select,
     build_head,
     PackedHead,
     logit_fidelity,
     lib,
+    matmul_i8,
     pack_int4,
     pack_int5,
     packed_bytes,
+    quantize_i8,
     unpack_int4,
     unpack_int5,
     validate_desc,

@@ -20,8 +20,9 @@ ABI_VERSION = 3
 OK, E_INVALID_ARG, E_MISALIGNED, E_UNSUPPORTED, E_WORKSPACE, E_HIP = range(6)
 F32, BF16, F16, I32, I64, I8, U8, I5 = range(8)
 INT4_V1 = 1
-OP_LOGITS, OP_LOGITS_CE, OP_ARGMAX, OP_TOPK, OP_FIDELITY = 0, 1, 2, 3, 4
+OP_LOGITS, OP_LOGITS_CE, OP_ARGMAX, OP_TOPK, OP_FIDELITY, OP_BEAM = 0, 1, 2, 3, 4, 5
 TOPK_MAX = 64
+BEAM_MAX = 32
 (LAUNCH_GEMV_BLOCKS_PER_CU, LAUNCH_GEMV_GRID, LAUNCH_DEC_BLOCKS, LAUNCH_MID_BLOCKS,
  LAUNCH_TILE_WAVES, LAUNCH_TILE_ROWS, LAUNCH_T_SPIN_LIMIT) = range(7)
 NOALLOC_SCRATCH_BYTES = 4 << 20   # ARCHEAD_NOALLOC_SCRATCH_BYTES of include/archead.h
@@ -62,6 +63,13 @@ class Ptrs(ctypes.Structure):
         "res_codes", "res_scales", "core_u", "core_u_scale", "core_v",
         "core_v_scale", "corr_a", "corr_a_scale", "corr_b", "corr_b_scale",
         "res_row_scales")]
+
+
+class StateLayout(ctypes.Structure):
+    """archead_state_layout: a row of a state, sizes and strides in bytes."""
+    _fields_ = [(n, ctypes.c_int64) for n in (
+        "n_outer", "positions", "pos_bytes", "src_row", "src_outer", "src_pos",
+        "dst_row", "dst_outer", "dst_pos")]
 
 
 _SIGS = {
@@ -108,6 +116,31 @@ _SIGS = {
                                           ctypes.c_void_p, ctypes.POINTER(Ptrs), ctypes.c_void_p,
                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                                           ctypes.c_void_p]),
+    "archead_quantize_i8": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64,
+                                           ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+    "archead_matmul_i8": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                         ctypes.c_int64, ctypes.c_void_p, ctypes.c_int,
+                                         ctypes.c_int64, ctypes.c_void_p]),
+    "archead_beam_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
+    "archead_beam_select": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64,
+                                           ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                           ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p]),
+    "archead_logits_beam": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                           ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                           ctypes.c_void_p]),
+    "archead_beam_reorder": (ctypes.c_int, [ctypes.POINTER(StateLayout), ctypes.c_int64,
+                                            ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                            ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]),
     "archead_set_gemv_max_m": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64]),
     "archead_get_gemv_max_m": (ctypes.c_int64, [ctypes.c_void_p]),
     "archead_set_dec_range": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64]),
@@ -263,6 +296,269 @@ def logit_fidelity(ref, test):
                                     _ptr(kl), _ptr(sq), _ptr(idx), _ptr(rank), _ptr(ws),
                                     ws.numel(), stream), L)
     return kl, sq, idx, rank
+
+
+def _float_code(dtype, what):
+    import torch
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16")
+    return code
+
+
+def _matrix(t, what, device, dtype=None, shape=None):
+    """The leading dimension of a 2-D tensor on `device` with unit column
+    stride (of a single row, one that holds the row)."""
+    if t.device != device or t.device.type != "cuda":
+        raise ValueError(f"{what} must be on {device if device.type == 'cuda' else 'a GPU'}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{what} must be 2-D" if shape is None else f"{what} must have shape {list(shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have unit column stride")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _dense(t, what, device, dtypes, shape):
+    """Checks a contiguous tensor of a shape and one of some dtypes on `device`."""
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous with shape {list(shape)}")
+
+
+def _launch(device, fn, *args):
+    """fn(*args, stream) with `device` the current one, on its current stream."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if st != OK:
+        _check(st)
+
+
+def quantize_i8(x, codes=None, scales=None):
+    """Rows of x (float32, bfloat16 or float16 [M, d] on the GPU) rounded to
+    8 bits: returns (codes int8 [M, d], scales float32 [M]) with x about codes *
+    scales[:, None] (archead_quantize_i8).  Rows are tokens, or the output
+    channels of a weight."""
+    import torch
+    dev = x.device
+    ldx = _matrix(x, "x", dev)
+    code = _float_code(x.dtype, "x")
+    M, d = x.shape
+    if codes is None:
+        codes = torch.empty((M, d), dtype=torch.int8, device=dev)
+    ldc = _matrix(codes, "codes", dev, torch.int8, (M, d))
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device=dev)
+    else:
+        _dense(scales, "scales", dev, (torch.float32,), (M,))
+    _launch(dev, lib().archead_quantize_i8, x.data_ptr(), code, M, d, ldx, codes.data_ptr(), ldc,
+            scales.data_ptr())
+    return codes, scales
+
+
+def matmul_i8(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=None):
+    """a int8 [M, K] x b int8 [N, K] -> out [M, N] = (a @ b.T) * a_scales[:,
+    None] * b_scales (+ bias), the sums in exact integers (archead_matmul_i8).
+    Scales and bias are float32; out is float32 (the default), bfloat16 or
+    float16."""
+    import torch
+    dev = a.device
+    lda = _matrix(a, "a", dev, torch.int8)
+    ldb = _matrix(b, "b", dev, torch.int8)
+    M, K = a.shape
+    N = b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError("a and b must have the same number of columns")
+    _dense(a_scales, "a_scales", dev, (torch.float32,), (M,))
+    _dense(b_scales, "b_scales", dev, (torch.float32,), (N,))
+    if bias is not None:
+        _dense(bias, "bias", dev, (torch.float32,), (N,))
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=dev)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out and out_dtype disagree")
+    ldo = _matrix(out, "out", dev, None, (M, N))
+    _launch(dev, lib().archead_matmul_i8, a.data_ptr(), lda, a_scales.data_ptr(), b.data_ptr(), ldb,
+            b_scales.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(),
+            _float_code(out.dtype, "out"), ldo)
+    return out
+
+
+def _beam_call(dev, V, scores, n, finished, end_token, ws, ws_bytes, call):
+    """Outputs and workspace of a beam selection, around call(...)."""
+    import torch
+    if scores.dim() != 2:
+        raise ValueError("scores must be [B, K]")
+    B, K = scores.shape
+    _dense(scores, "scores", dev, (torch.float32,), (B, K))
+    if finished is not None:
+        _dense(finished, "finished", dev, (torch.bool, torch.uint8), (B, K))
+    n = int(n)
+    if not 1 <= n <= TOPK_MAX:
+        raise ValueError(f"n must be in 1 .. {TOPK_MAX}")
+    out = torch.empty((B, n), dtype=torch.float32, device=dev)
+    pair = torch.empty((2, B, n), dtype=torch.int64, device=dev)
+    parents, tokens = pair[0], pair[1]
+    ended = torch.empty((B, n), dtype=torch.bool, device=dev) if end_token >= 0 else None
+    need = ws_bytes(B * K)
+    if ws is None:
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous uint8 tensor on the same device")
+    call(B, K, _ptr(scores), _ptr(finished), int(end_token), n, _ptr(out), _ptr(parents), _ptr(tokens),
+         _ptr(ended), _ptr(ws), ws.numel())
+    return (out, parents, tokens) if ended is None else (out, parents, tokens, ended)
+
+
+def beam_select(logits, scores, n, finished=None, end_token=-1, ws=None):
+    """The n best continuations of each sequence of a beam search
+    (archead_beam_select).  logits: float32, bfloat16 or float16 [B * K, V],
+    row b * K + k for beam k of sequence b; scores: float32 [B, K], the beams'
+    summed log-probabilities (-inf: a beam not in use); finished: bool [B, K] or
+    None, beams that ended (they offer end_token with their score unchanged).
+    Returns (scores float32 [B, n], parents int64 [B, n], tokens int64 [B,
+    n]), best first, and with an end_token also which of them have ended, bool
+    [B, n].  Empty places hold (-inf, -1, -1)."""
+    dev = logits.device
+    ldl = _matrix(logits, "logits", dev)
+    code = _float_code(logits.dtype, "logits")
+    R, V = logits.shape
+    if scores.numel() != R:
+        raise ValueError("logits must have a row for every beam of scores")
+    L = lib()
+
+    def call(B, K, *rest):
+        _launch(dev, L.archead_beam_select, logits.data_ptr(), code, B, K, V, ldl, *rest)
+    return _beam_call(dev, V, scores, n, finished, end_token, ws,
+                      lambda rows: L.archead_beam_workspace_bytes(rows, V), call)
+
+
+class BeamStates:
+    """The states of a beam search's rows (caches of every layer, recurrent
+    states, token histories), described once and reordered after every step
+    (archead_beam_reorder).
+
+    states: tensors on one GPU of beams * B rows along `row_dim`.  out: tensors
+    for the reordered states, of out_beams * B rows (default: beams) and
+    otherwise alike, sharing no memory with states; or None to reorder the
+    states where they are.  pos_dim: the dimension of the positions, where
+    reorder() is to move the leading ones alone.  Of the remaining dimensions,
+    those that do not lie back to back have to step as one."""
+
+    def __init__(self, states, beams, out=None, out_beams=None, row_dim=0, pos_dim=None):
+        states = list(states)
+        self.states, self.beams = states, int(beams)
+        self.in_place = out is None
+        self.out = states if out is None else list(out)
+        self.out_beams = self.beams if out_beams is None else int(out_beams)
+        if len(self.out) != len(states):
+            raise ValueError("as many out tensors as states are needed")
+        if not 1 <= self.beams <= BEAM_MAX or not 1 <= self.out_beams <= TOPK_MAX:
+            raise ValueError(f"beams must be in 1 .. {BEAM_MAX} and out_beams in 1 .. {TOPK_MAX}")
+        if self.in_place and self.out_beams != self.beams:
+            raise ValueError("reordering in place keeps the number of beams")
+        self.has_pos = pos_dim is not None
+        self.batch = self.device = None
+        groups = {}
+        for i, (s, d) in enumerate(zip(states, self.out)):
+            if s.device.type != "cuda" or d.device != s.device or (self.device or s.device) != s.device:
+                raise ValueError("states and out must be on one GPU")
+            self.device = s.device
+            if s.dim() == 0 or not -s.dim() <= row_dim < s.dim():
+                raise ValueError("states must have a dimension row_dim")
+            r = row_dim % s.dim()
+            p = None if pos_dim is None else pos_dim % s.dim()
+            if pos_dim is not None and (not -s.dim() <= pos_dim < s.dim() or p == r):
+                raise ValueError("pos_dim must be a dimension of the states other than row_dim")
+            if s.dtype != d.dtype or s.dim() != d.dim() or any(
+                    s.shape[k] != d.shape[k] for k in range(s.dim()) if k != r):
+                raise ValueError("out must have the states' dtype and, but for rows, their shape")
+            B = s.shape[r] // self.beams
+            if s.shape[r] != B * self.beams or d.shape[r] != B * self.out_beams or B != (self.batch or B):
+                raise ValueError("states must have beams * B rows, out must have out_beams * B")
+            self.batch = B
+            key = self._layout(s, d, r, p)
+            if d.numel():
+                groups.setdefault(key, []).append(i)
+        starts = [t.data_ptr() for t in self.out if t.numel()]
+        if len(set(starts)) != len(starts):
+            raise ValueError("two of the destinations are the same memory")
+        if not self.in_place:
+            spans = sorted([(*self._span(t), w) for w, ts in ((0, states), (1, self.out)) for t in ts if t.numel()])
+            ends = [-1, -1]
+            for lo, hi, w in spans:
+                if lo < ends[1 - w]:
+                    raise ValueError("out shares memory with states")
+                ends[w] = max(ends[w], hi)
+        self._groups = []
+        for key, members in groups.items():
+            arr = ctypes.c_void_p * len(members)
+            self._groups.append((StateLayout(*key), len(members), arr(*[states[i].data_ptr() for i in members]),
+                                 arr(*[self.out[i].data_ptr() for i in members])))
+
+    @staticmethod
+    def _span(t):
+        lo = t.data_ptr()
+        return lo, lo + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size()
+
+    @staticmethod
+    def _layout(s, d, r, p):
+        """archead_state_layout of a state and its destination, as a tuple."""
+        es = s.element_size()
+        # (size, stride of s, stride of d) of the dimensions, smallest steps first
+        dims = [(s.shape[k], s.stride(k) * es, d.stride(k) * es) for k in range(s.dim())
+                if k not in (r, p) and s.shape[k] != 1]
+        dims.sort(key=lambda t: (t[2], t[1]))
+        inner, outer = es, (1, 0, 0)
+        for n, a, b in dims:
+            if outer[0] == 1 and a == inner and b == inner:
+                inner *= n
+            elif outer[0] == 1:
+                outer = (n, a, b)
+            elif a == outer[0] * outer[1] and b == outer[0] * outer[2]:
+                outer = (outer[0] * n, outer[1], outer[2])
+            else:
+                raise ValueError("the dimensions of a state that do not lie back to back must step as one")
+        rows = (d.shape[r], s.stride(r) * es, d.stride(r) * es)
+        pos = (1, 0, 0) if p is None else (s.shape[p], s.stride(p) * es, d.stride(p) * es)
+        # a destination's elements are its own: each step passes all smaller ones
+        end = inner
+        for n, _, b in sorted((outer, pos, rows), key=lambda t: t[2]):
+            if n > 1:
+                if b < end:
+                    raise ValueError("elements of a destination share memory")
+                end = b * (n - 1) + end
+        return (outer[0], pos[0], inner, rows[1], outer[1], pos[1], rows[2], outer[2], pos[2])
+
+    def reorder(self, parents, lengths=None):
+        """Row b * out_beams + j becomes row b * beams + parents[b, j] of the
+        states; parents outside [0, beams) leave it as it is.  parents: int64 or
+        int32 [B, out_beams].  lengths: int32 [B] or None; positions from
+        lengths[b] on stay as they are.  Returns the destinations, on the
+        current stream."""
+        import torch
+        if not self._groups:
+            return self.out
+        B, n = self.batch, self.out_beams
+        _dense(parents, "parents", self.device, (torch.int64, torch.int32), (B, n))
+        if lengths is not None:
+            if not self.has_pos:
+                raise ValueError("lengths need pos_dim")
+            _dense(lengths, "lengths", self.device, (torch.int32,), (B,))
+        idx = I64 if parents.dtype == torch.int64 else I32
+        fn = lib().archead_beam_reorder
+        for layout, count, src, dst in self._groups:
+            _launch(self.device, fn, layout, count, src, dst, B, self.beams, n, parents.data_ptr(), idx,
+                    _ptr(lengths))
+        return self.out
 
 
 def build_head(W, H, rc: int, rr: int, g: int, p: float = 0.75, lam: float = 1e-3, gB=None,
@@ -536,6 +832,20 @@ class PackedHead:
             self.handle, _ptr(x), M, x.stride(0), int(k), _ptr(vals), _ptr(idx), idx.stride(0),
             _ptr(ws), ws.numel(), self._stream(x.device)), self._lib)
         return vals, idx
+
+    def logits_beam(self, x, scores, n, finished=None, end_token=-1, ws=None):
+        """beam_select over this head's logits of the beams' hidden states x,
+        bf16 [B * K, d] (archead_logits_beam)."""
+        import torch
+        dev = x.device
+        ldx = _matrix(x, "x", dev, torch.bfloat16)
+        if x.shape[1] != self.d or scores.numel() != x.shape[0]:
+            raise ValueError("x must have d columns and a row for every beam of scores")
+
+        def call(B, K, *rest):
+            _launch(dev, self._lib.archead_logits_beam, self.handle, x.data_ptr(), B, K, ldx, *rest)
+        return _beam_call(dev, self.V, scores, n, finished, end_token, ws,
+                          lambda rows: self.workspace_bytes(rows, OP_BEAM), call)
 
     def logit_fidelity_head(self, x, dense, ws=None):
         """Fidelity of this head to a dense bf16 head [V, d] on the tokens x,

@@ -31,6 +31,7 @@
 
 #include "archead.h"
 #include "internal.h"
+#include "beam.h"
 #include "kernels.h"
 #include "dev_gemv.cuh"
 #include "dev_dec.cuh"
@@ -358,6 +359,12 @@ static WsLayout topk_layout(const archead_handle* h, int64_t M) {
 
 WsLayout ws_layout(const archead_handle* h, int64_t M, archead_op op) {
   if (h && M > 0 && op == ARCHEAD_OP_TOPK) return topk_layout(h, M);
+  if (h && M > 0 && op == ARCHEAD_OP_BEAM) {   // the logits, then either call's workspace
+    WsLayout w = ws_layout(h, M, ARCHEAD_OP_LOGITS);
+    w.total = round256(sizeof(float) * size_t(M) * size_t(h->desc.V)) +
+              std::max(round256(w.total), beam_layout(M, h->desc.V).total);
+    return w;
+  }
   if (h && M > 0 && op == ARCHEAD_OP_FIDELITY) {
     WsLayout w = ws_layout_path(h, M, ARCHEAD_OP_LOGITS, Path::kTiled);
     const size_t n_vt = size_t((h->desc.V + kTN - 1) / kTN);

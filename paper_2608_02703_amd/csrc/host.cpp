@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "beam.h"
 #include "internal.h"
 
 namespace archead {
@@ -153,6 +154,61 @@ Path choose_path(const archead_handle* h, int64_t M) {
   if (use_mid(h, M)) return Path::kMid;
   if (use_gemv(h, M)) return Path::kGemv;
   return Path::kTiled;
+}
+
+static bool off(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+archead_status beam_check(int64_t B, int64_t K, int64_t V, const float* scores, const uint8_t* finished,
+                          int64_t end_token, int32_t n, const float* out_scores, const int64_t* parents,
+                          const int64_t* tokens) {
+  if (K < 1 || K > ARCHEAD_BEAM_MAX)
+    return fail(ARCHEAD_E_INVALID_ARG, "K = %lld is outside 1 .. %d", (long long)K, ARCHEAD_BEAM_MAX);
+  if (B < 0 || B > 65535 / K) return fail(ARCHEAD_E_INVALID_ARG, "B = %lld out of range (B K <= 65535)", (long long)B);
+  if (V < 1 || V > INT32_MAX) return fail(ARCHEAD_E_INVALID_ARG, "V = %lld out of range", (long long)V);
+  if (n < 1 || n > kTopKMaxK) return fail(ARCHEAD_E_INVALID_ARG, "n = %d is outside 1 .. %d", int(n), kTopKMaxK);
+  if (end_token < -1 || end_token >= V)
+    return fail(ARCHEAD_E_INVALID_ARG, "end_token = %lld is outside -1 .. V - 1", (long long)end_token);
+  if (finished && end_token < 0) return fail(ARCHEAD_E_INVALID_ARG, "finished needs an end_token");
+  if (B == 0) return ARCHEAD_OK;
+  if (!scores || !out_scores || !parents || !tokens) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
+  if (off(scores, 4) || off(out_scores, 4) || off(parents, 8) || off(tokens, 8))
+    return fail(ARCHEAD_E_MISALIGNED, "scores / out_scores / parents / tokens misaligned");
+  return ARCHEAD_OK;
+}
+
+archead_status reorder_check(const archead_state_layout* l, int64_t n_states, const void* const* src,
+                             void* const* dst, int64_t B, int64_t K, int64_t n, const void* parents,
+                             archead_dtype idx_dtype, const int32_t* lengths, bool* in_place) {
+  if (!l) return fail(ARCHEAD_E_INVALID_ARG, "layout is NULL");
+  if (K < 1 || K > ARCHEAD_BEAM_MAX)
+    return fail(ARCHEAD_E_INVALID_ARG, "K = %lld is outside 1 .. %d", (long long)K, ARCHEAD_BEAM_MAX);
+  if (n < 1 || n > kTopKMaxK) return fail(ARCHEAD_E_INVALID_ARG, "n = %lld is outside 1 .. %d", (long long)n, kTopKMaxK);
+  if (B < 0 || B >= (int64_t(1) << 31) / kTopKMaxK) return fail(ARCHEAD_E_INVALID_ARG, "B = %lld out of range", (long long)B);
+  if (n_states < 0) return fail(ARCHEAD_E_INVALID_ARG, "n_states = %lld", (long long)n_states);
+  if (idx_dtype != ARCHEAD_I32 && idx_dtype != ARCHEAD_I64)
+    return fail(ARCHEAD_E_INVALID_ARG, "idx_dtype must be I32 or I64");
+  // sizes that keep every product below 2^63
+  const int64_t sizes[] = {l->n_outer, l->positions, l->pos_bytes, l->src_row, l->src_outer,
+                           l->src_pos, l->dst_row, l->dst_outer, l->dst_pos};
+  for (int i = 0; i < 9; ++i)
+    if (sizes[i] < 0 || sizes[i] > (int64_t(1) << (i < 3 ? 31 : 42)))
+      return fail(ARCHEAD_E_INVALID_ARG, "a size or stride of the layout is out of range (%lld)", (long long)sizes[i]);
+  if (double(l->n_outer) * double(l->positions) * double(l->pos_bytes) > 0x1p45)
+    return fail(ARCHEAD_E_INVALID_ARG, "a row of more than 2^45 bytes");
+  if (n_states == 0 || B == 0) return ARCHEAD_OK;
+  if (!src || !dst || !parents) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
+  int64_t same = 0;
+  for (int64_t i = 0; i < n_states; ++i) {
+    if (!src[i] || !dst[i]) return fail(ARCHEAD_E_INVALID_ARG, "state %lld is a null pointer", (long long)i);
+    same += src[i] == dst[i];
+  }
+  if (same && same != n_states) return fail(ARCHEAD_E_INVALID_ARG, "some states in place, others not");
+  *in_place = same != 0;
+  if (same && (n != K || l->src_row != l->dst_row || l->src_outer != l->dst_outer || l->src_pos != l->dst_pos))
+    return fail(ARCHEAD_E_INVALID_ARG, "in place needs n == K and the same strides");
+  if (off(parents, idx_dtype == ARCHEAD_I64 ? 8 : 4) || off(lengths, 4))
+    return fail(ARCHEAD_E_MISALIGNED, "parents / lengths misaligned");
+  return ARCHEAD_OK;
 }
 
 }  // namespace archead

@@ -1,0 +1,169 @@
+// archead_matmul_i8: products of 8-bit integers with a scale per row of each
+// operand.
+//
+// v_mfma_i32_16x16x64_i8: lane l holds 16 consecutive k of row l % 16 of an
+// operand, from 16 (l / 16) on; of the result column l % 16 (second operand)
+// and rows 4 (l / 16) .. + 3 (first operand).  The channels (b) go first, so a
+// lane ends with four neighbouring channels of one token.
+#include "dev_rows.cuh"
+
+namespace {
+
+using namespace archead::rows;
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+struct I8Args {
+  const int8_t* a;
+  const int8_t* b;
+  const float* sa;
+  const float* sb;
+  const float* bias;   // may be null
+  uint8_t* out;
+  int64_t lda, ldb, ldo;
+  int64_t M, N;
+  int K;
+};
+
+// four neighbouring outputs of a token
+template <int DT>
+__device__ __forceinline__ void store4(uint8_t* p, const float (&y)[4], int n) {
+  if constexpr (DT == ARCHEAD_F32) {
+    if (n == 4) {
+      store_any(p, float4{y[0], y[1], y[2], y[3]});
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) reinterpret_cast<float*>(p)[i] = y[i];
+  } else {
+    uint16_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (DT == ARCHEAD_BF16) h[i] = bf16_rne(y[i]);
+      else {
+        const _Float16 f = _Float16(y[i]);
+        __builtin_memcpy(&h[i], &f, 2);
+      }
+    }
+    if (n == 4) {
+      store_any(p, uint2{h[0] | uint32_t(h[1]) << 16, h[2] | uint32_t(h[3]) << 16});
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) reinterpret_cast<uint16_t*>(p)[i] = h[i];
+  }
+}
+
+// the outputs of channels n .. n + 3 of token m
+template <int DT>
+__device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, const i32x4& acc) {
+  if (m >= g.M || n >= g.N) return;
+  const int cnt = g.N - n < 4 ? int(g.N - n) : 4;
+  const float s = g.sa[m];
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t c = i < cnt ? n + i : n;
+    y[i] = float(acc[i]) * s * g.sb[c];
+    if (g.bias) y[i] += g.bias[c];
+  }
+  store4<DT>(g.out + (m * g.ldo + n) * (DT == ARCHEAD_F32 ? 4 : 2), y, cnt);
+}
+
+// ---------------------------------------------- any alignment, any K
+// Tiles of 64 tokens x 64 channels, 128 of k at a time through registers into
+// LDS, bytes past K as zeros.  Four waves of 32 x 32.
+constexpr int kABlock = 256, kATile = 64, kAK = 128, kAStride = kAK + 16;
+
+template <int DT>
+__global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, int64_t tiles) {
+  __shared__ __align__(16) int8_t lds[2][kATile * kAStride];
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int wm = (wid & 1) * 32, wn = (wid >> 1) * 32;
+  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int64_t m0 = (t % m_tiles) * kATile, n0 = (t / m_tiles) * kATile;
+    i32x4 acc[2][2] = {};
+    for (int k0 = 0; k0 < g.K; k0 += kAK) {
+      uint4 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {   // two pieces of a's tile, two of b's
+        const int piece = tid + (i & 1) * kABlock, row = piece / 8, k = k0 + (piece % 8) * 16;
+        const int64_t r = (i < 2 ? m0 : n0) + row;
+        const int8_t* p = i < 2 ? g.a + r * g.lda + k : g.b + r * g.ldb + k;
+        w[i] = uint4{0, 0, 0, 0};
+        if (r < (i < 2 ? g.M : g.N)) {
+          if (k + 16 <= g.K) w[i] = load_any<uint4>(p);
+          else {
+            uint32_t d[4] = {};
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (k + j < g.K) d[j / 4] |= uint32_t(uint8_t(p[j])) << (8 * (j % 4));
+            w[i] = uint4{d[0], d[1], d[2], d[3]};
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int piece = tid + (i & 1) * kABlock;
+        *reinterpret_cast<uint4*>(&lds[i / 2][(piece / 8) * kAStride + (piece % 8) * 16]) = w[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int kk = 0; kk < kAK; kk += 64) {
+        i32x4 fa[2], fb[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = (lane & 15) * kAStride + kk + (lane >> 4) * 16;
+          fa[i] = *reinterpret_cast<const i32x4*>(&lds[0][(wm + 16 * i) * kAStride + at]);
+          fb[i] = *reinterpret_cast<const i32x4*>(&lds[1][(wn + 16 * i) * kAStride + at]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        finish4<DT>(g, m0 + wm + 16 * i + (lane & 15), n0 + wn + 16 * j + 4 * (lane >> 4), acc[i][j]);
+  }
+}
+
+template <int DT>
+void launch_matmul(const I8Args& g, hipStream_t s) {
+  const int64_t mt = (g.M + kATile - 1) / kATile, nt = (g.N + kATile - 1) / kATile, tiles = mt * nt;
+  const dim3 grid{unsigned(tiles < (1 << 22) ? tiles : 1 << 22)};
+  hipLaunchKernelGGL(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
+}
+
+}  // namespace
+
+extern "C" archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const float* a_scales, const int8_t* b,
+                                            int64_t ldb, const float* b_scales, const float* bias, int64_t M,
+                                            int64_t N, int64_t K, void* out, archead_dtype out_dtype, int64_t ldo,
+                                            void* stream) {
+  using archead::fail;
+  archead::clear_error();
+  if (!float_dtype(out_dtype)) return fail(ARCHEAD_E_INVALID_ARG, "out_dtype must be F32, BF16 or F16");
+  if (M < 0 || M > INT32_MAX || N < 0 || N > INT32_MAX || K < 0)
+    return fail(ARCHEAD_E_INVALID_ARG, "M = %lld, N = %lld, K = %lld out of range", (long long)M, (long long)N,
+                (long long)K);
+  // 2^31 / 128^2: the largest sum of K products of codes stays below 2^31
+  if (K > 131071) return fail(ARCHEAD_E_UNSUPPORTED, "K = %lld > 131071: the sum may pass 32 bits", (long long)K);
+  if (M == 0 || N == 0) return ARCHEAD_OK;
+  if (lda < K || ldb < K || ldo < N) return fail(ARCHEAD_E_INVALID_ARG, "leading dimensions must be >= K and N");
+  if ((K && (!a || !b)) || !a_scales || !b_scales || !out) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
+  if (!aligned(a_scales, 4) || !aligned(b_scales, 4) || !aligned(bias, 4) || !aligned(out, dtype_bytes(out_dtype)))
+    return fail(ARCHEAD_E_MISALIGNED, "scales / bias / out misaligned");
+  const I8Args g{a, b, a_scales, b_scales, bias, static_cast<uint8_t*>(out), lda, ldb, ldo, M, N, int(K)};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (out_dtype == ARCHEAD_F32) launch_matmul<ARCHEAD_F32>(g, s);
+  else if (out_dtype == ARCHEAD_BF16) launch_matmul<ARCHEAD_BF16>(g, s);
+  else launch_matmul<ARCHEAD_F16>(g, s);
+  return launch_status(hipGetLastError(), "int8 product launch");
+}
