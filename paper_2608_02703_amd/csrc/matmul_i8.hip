@@ -1,76 +1,10 @@
 // archead_matmul_i8: products of 8-bit integers with a scale per row of each
 // operand.
-//
-// v_mfma_i32_16x16x64_i8: lane l holds 16 consecutive k of row l % 16 of an
-// operand, from 16 (l / 16) on; of the result column l % 16 (second operand)
-// and rows 4 (l / 16) .. + 3 (first operand).  The channels (b) go first, so a
-// lane ends with four neighbouring channels of one token.
-#include "dev_rows.cuh"
+#include "i8.cuh"
 
 namespace {
 
-using namespace archead::rows;
-
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-struct I8Args {
-  const int8_t* a;
-  const int8_t* b;
-  const float* sa;
-  const float* sb;
-  const float* bias;   // may be null
-  uint8_t* out;
-  int64_t lda, ldb, ldo;
-  int64_t M, N;
-  int K;
-};
-
-// four neighbouring outputs of a token
-template <int DT>
-__device__ __forceinline__ void store4(uint8_t* p, const float (&y)[4], int n) {
-  if constexpr (DT == ARCHEAD_F32) {
-    if (n == 4) {
-      store_any(p, float4{y[0], y[1], y[2], y[3]});
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) reinterpret_cast<float*>(p)[i] = y[i];
-  } else {
-    uint16_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (DT == ARCHEAD_BF16) h[i] = bf16_rne(y[i]);
-      else {
-        const _Float16 f = _Float16(y[i]);
-        __builtin_memcpy(&h[i], &f, 2);
-      }
-    }
-    if (n == 4) {
-      store_any(p, uint2{h[0] | uint32_t(h[1]) << 16, h[2] | uint32_t(h[3]) << 16});
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) reinterpret_cast<uint16_t*>(p)[i] = h[i];
-  }
-}
-
-// the outputs of channels n .. n + 3 of token m
-template <int DT>
-__device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, const i32x4& acc) {
-  if (m >= g.M || n >= g.N) return;
-  const int cnt = g.N - n < 4 ? int(g.N - n) : 4;
-  const float s = g.sa[m];
-  float y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t c = i < cnt ? n + i : n;
-    y[i] = float(acc[i]) * s * g.sb[c];
-    if (g.bias) y[i] += g.bias[c];
-  }
-  store4<DT>(g.out + (m * g.ldo + n) * (DT == ARCHEAD_F32 ? 4 : 2), y, cnt);
-}
+using namespace archead::i8;
 
 // ---------------------------------------------- any alignment, any K
 // Tiles of 64 tokens x 64 channels, 128 of k at a time through registers into
@@ -136,6 +70,7 @@ __global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, i
 
 template <int DT>
 void launch_matmul(const I8Args& g, hipStream_t s) {
+  if (tiles_take(g)) return launch_tiles<DT>(g, s);
   const int64_t mt = (g.M + kATile - 1) / kATile, nt = (g.N + kATile - 1) / kATile, tiles = mt * nt;
   const dim3 grid{unsigned(tiles < (1 << 22) ? tiles : 1 << 22)};
   hipLaunchKernelGGL(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
