@@ -28,34 +28,39 @@ struct I8Args {
   int K;
 };
 
-// four neighbouring outputs of a token
+// an output before its last rounding
+__device__ __forceinline__ float scaled(int acc, float sa, float sb, float bias, bool with_bias) {
+  const float y = float(acc) * sa * sb;
+  return with_bias ? y + bias : y;
+}
+
+// four fp32 values to the output's type, at p
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
 template <int DT>
-__device__ __forceinline__ void store4(uint8_t* p, const float (&y)[4], int n) {
-  if constexpr (DT == ARCHEAD_F32) {
-    if (n == 4) {
-      store_any(p, float4{y[0], y[1], y[2], y[3]});
-      return;
-    }
+__device__ __forceinline__ void put4(uint8_t* p, const float (&y)[4]) {
+  const f32x4v v{y[0], y[1], y[2], y[3]};
+  if constexpr (DT == ARCHEAD_F32) *reinterpret_cast<f32x4v*>(p) = v;
+  else if constexpr (DT == ARCHEAD_BF16) *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4);
+  else *reinterpret_cast<f16x4*>(p) = __builtin_convertvector(v, f16x4);
+}
+
+// the first `left` (at least all that fit) elements of EB bytes of v, at any address
+template <int EB, typename V>
+__device__ __forceinline__ void store_part(uint8_t* p, const V& v, int64_t left) {
+  constexpr int PER = sizeof(V) / EB;
+  if (left >= PER) {
+    store_any(p, v);
+    return;
+  }
+  uint32_t w[sizeof(V) / 4];
+  __builtin_memcpy(w, &v, sizeof(V));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) reinterpret_cast<float*>(p)[i] = y[i];
-  } else {
-    uint16_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (DT == ARCHEAD_BF16) h[i] = bf16_rne(y[i]);
-      else {
-        const _Float16 f = _Float16(y[i]);
-        __builtin_memcpy(&h[i], &f, 2);
-      }
-    }
-    if (n == 4) {
-      store_any(p, uint2{h[0] | uint32_t(h[1]) << 16, h[2] | uint32_t(h[3]) << 16});
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) reinterpret_cast<uint16_t*>(p)[i] = h[i];
+  for (int i = 0; i < PER; ++i) {
+    if (i >= left) continue;
+    if constexpr (EB == 4) *reinterpret_cast<uint32_t*>(p + 4 * i) = w[i];
+    else *reinterpret_cast<uint16_t*>(p + 2 * i) = uint16_t(w[i / 2] >> (16 * (i & 1)));
   }
 }
 
@@ -63,22 +68,23 @@ __device__ __forceinline__ void store4(uint8_t* p, const float (&y)[4], int n) {
 template <int DT>
 __device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, const i32x4& acc) {
   if (m >= g.M || n >= g.N) return;
-  const int cnt = g.N - n < 4 ? int(g.N - n) : 4;
+  constexpr int EB = DT == ARCHEAD_F32 ? 4 : 2;
   const float s = g.sa[m];
   float y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t c = i < cnt ? n + i : n;
-    y[i] = float(acc[i]) * s * g.sb[c];
-    if (g.bias) y[i] += g.bias[c];
+    const int64_t c = n + i < g.N ? n + i : n;
+    y[i] = scaled(acc[i], s, g.sb[c], g.bias ? g.bias[c] : 0.f, g.bias != nullptr);
   }
-  store4<DT>(g.out + (m * g.ldo + n) * (DT == ARCHEAD_F32 ? 4 : 2), y, cnt);
+  uint32_t w[EB];
+  put4<DT>(reinterpret_cast<uint8_t*>(w), y);
+  if constexpr (EB == 4) store_part<EB>(g.out + (m * g.ldo + n) * EB, uint4{w[0], w[1], w[2], w[3]}, g.N - n);
+  else store_part<EB>(g.out + (m * g.ldo + n) * EB, uint2{w[0], w[1]}, g.N - n);
 }
-
 
 // kernel launchers, one translation unit each
 template <int DT>
-void launch_tiles(const I8Args& g, hipStream_t s);   // a, b aligned to 16, K, lda, ldb multiples of 16
+void launch_tiles(const I8Args& g, int n_cu, hipStream_t s);   // a, b aligned to 16, K, lda, ldb multiples of 16
 bool tiles_take(const I8Args& g);
 
 }  // namespace i8

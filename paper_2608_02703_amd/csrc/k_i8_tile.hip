@@ -1,4 +1,4 @@
-// archead_matmul_i8 for many tokens: tiles of TM tokens x 256 channels.
+// archead_matmul_i8 for several tokens: tiles of TM tokens x 256 channels.
 #include "dev_common.cuh"
 #include "i8.cuh"
 
@@ -8,189 +8,312 @@ using namespace archead::i8;
 
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTK = 128;          // k of a stage
 constexpr int kTileN = 256;       // channels of a tile
 constexpr int kRaster = 8;        // token tiles of a raster group
 constexpr int kMaxLd = 1 << 22;   // a tile's rows stay within 31-bit offsets
 
-template <int TM, int WMW, int WNW>
+// NS stages in LDS, WMW x WNW waves
+template <int TM, int WMW, int WNW, int NS>
 struct Geom {
-  static constexpr int NW = WMW * WNW;                     // waves
+  static constexpr int NW = WMW * WNW;
   static constexpr int WM = TM / WMW, WN = kTileN / WNW;   // a wave's tokens, channels
   static constexpr int MI = WM / 32, NI = WN / 32;
   static constexpr int ABYTES = TM * kTK, STAGE = ABYTES + kTileN * kTK;
   static constexpr int NA = ABYTES / 1024 / NW, NB = kTileN * kTK / 1024 / NW;   // loads of a wave and stage
-  static constexpr int LDS = 2 * STAGE;
-  static constexpr int OUT = WN + 4;                       // floats of a token in a wave's store buffer
-  static_assert(NW * 32 * OUT * 4 <= LDS && LDS <= 160 * 1024, "LDS budget");
+  static constexpr int OROW = 80, OUT = NS * STAGE;        // a wave's store buffer: 32 tokens of 64 bytes, padded
+  static constexpr int SCALES = OUT + NW * 32 * OROW;      // fp32 [2][TM + 2 kTileN]: a_scales, b_scales, bias
+  static constexpr int NSC = TM + 2 * kTileN;
+  static constexpr int LDS = SCALES + 2 * NSC * 4;
+  static_assert(LDS <= 160 * 1024, "LDS budget");
   static_assert(NA * 1024 * NW == ABYTES && NB * 1024 * NW == kTileN * kTK, "whole loads");
 };
 
-// Two stages of 128 k in LDS: one computed, one on its way.  Rows of 128 bytes
-// with their 16-byte units swizzled, so eight rows' reads of one unit fall on
-// eight different bank groups.  A wave reads the operands of a K-step (32 k)
-// during the step before.  Before the last step of a stage all its reads are
-// done, so there the waves meet, once a stage: the next stage has landed, its
-// first operands are read and the loads of the one after it overwrite this
-// one, all under the last step's products.
-template <int DT, int TM, int WMW, int WNW>
-__global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_i8_tile(
-    I8Args g, int m_tiles, int n_tiles, int64_t per_xcd) {
-  using G = Geom<TM, WMW, WNW>;
+// The order of a K-step of P products: after each of the first ones a share of
+// R LDS reads, one or two, and of V loads to LDS.  Without it the compiler puts
+// the next step's reads right before their use.
+template <int R, int V, int P, int I = 0>
+__device__ __forceinline__ void spread() {
+  if constexpr (I < P) {
+    constexpr int H = P * 3 / 4 > 0 ? P * 3 / 4 : 1;
+    constexpr int r = I < H ? R * (I + 1) / H - R * I / H : 0, v = V * (I + 1) / P - V * I / P;
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);   // products
+    if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    if constexpr (v > 0) __builtin_amdgcn_sched_group_barrier(0x10, v, 0);
+    spread<R, V, P, I + 1>();
+  } else {
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// LDS accesses of one wave stay in this order (the hardware keeps it; lanes
+// read what other lanes wrote, which the compiler does not see).
+__device__ __forceinline__ void wave_lds_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A persistent workgroup per CU takes its XCD's tiles in turn, their stages as
+// one sequence: the loads run NS stages ahead of the products, across tiles,
+// so the next tile's first stages are on their way while one tile is written.
+//
+// LDS rows of 128 bytes have their 16-byte units swizzled, so eight rows' reads
+// of one unit fall on eight different bank groups.  A wave reads the operands
+// of a K-step (32 k) during the step before.  Before the last step of a stage
+// all its reads are done, so there the waves meet, once a stage: the next stage
+// has landed, its first operands are read and later loads overwrite this one,
+// all under the last step's products.
+template <int DT, int TM, int WMW, int WNW, int NS>
+__global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(WMW * WNW / 4))) void k_i8_tile(
+    I8Args g, int m_tiles, int n_tiles, int per_xcd) {
+  using G = Geom<TM, WMW, WNW, NS>;
   constexpr int MI = G::MI, NI = G::NI;
   extern __shared__ __align__(16) uint8_t i8_lds[];
   lds_u8* const L = (lds_u8*)i8_lds;
-
-  // workgroups go to the 8 XCDs in turn; each XCD takes a contiguous run of
-  // the order that walks groups of kRaster token tiles along the channels
-  const int64_t lin = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (lin >= int64_t(m_tiles) * n_tiles) return;
-  const int64_t gsz = int64_t(kRaster) * n_tiles, rg = lin / gsz;
-  const int first = int(rg) * kRaster, gm = min(m_tiles - first, kRaster), within = int(lin - rg * gsz);
-  const int64_t m0 = int64_t(first + within % gm) * TM, n0 = int64_t(within / gm) * kTileN;
-  const int rows = int(g.M - m0 < TM ? g.M - m0 : TM), cols = int(g.N - n0 < kTileN ? g.N - n0 : kTileN);
-
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wid / WNW, wn = wid % WNW;
   const int lda = int(g.lda), ldb = int(g.ldb);
-  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<int8_t*>(g.a + m0 * g.lda), 0, (rows - 1) * lda + g.K, kBufferWord3);
-  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<int8_t*>(g.b + n0 * g.ldb), 0, (cols - 1) * ldb + g.K, kBufferWord3);
+  const int stages = (g.K + kTK - 1) / kTK;
 
+  // workgroups go to the 8 XCDs in turn; each XCD takes a contiguous run of
+  // the order that walks groups of kRaster token tiles along the channels
+  const int n_all = m_tiles * n_tiles, x0 = int(blockIdx.x & 7) * per_xcd;
+  const int end = min(per_xcd, n_all - x0), step = int(gridDim.x >> 3);
+  int cur = int(blockIdx.x >> 3);
+  if (cur >= end) return;
+  auto tile_at = [&](int t, int& m0, int& n0) {
+    const int lin = x0 + t, gsz = kRaster * n_tiles, rg = lin / gsz, first = rg * kRaster;
+    const int gm = min(m_tiles - first, kRaster), within = lin - rg * gsz;
+    m0 = (first + within % gm) * TM;
+    n0 = within / gm * kTileN;
+  };
+
+  // ---- loads: the tile and stage they have come to
+  int ld_tile = cur, ld_stage = 0, ld_slot = 0;
+  __amdgpu_buffer_rsrc_t ra, rb;
+  uint32_t ao[G::NA], bo[G::NB];
   // this lane's unit of its wave's load i: row r, unit p of LDS, holding unit
   // p ^ swz of the row; rows past the last repeat it
-  uint32_t ao[G::NA], bo[G::NB];
-#pragma unroll
-  for (int i = 0; i < G::NA; ++i) {
-    const int off = (wid * G::NA + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-    ao[i] = uint32_t(min(r, rows - 1)) * lda + 16 * (p ^ swz_x(r));
-  }
-#pragma unroll
-  for (int i = 0; i < G::NB; ++i) {
-    const int off = (wid * G::NB + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-    bo[i] = uint32_t(min(r, cols - 1)) * ldb + 16 * (p ^ swz_x(r));
-  }
-  const int stages = (g.K + kTK - 1) / kTK;
-  auto load = [&](__amdgpu_buffer_rsrc_t r, lds_u8* dst, uint32_t off, int k0) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, reinterpret_cast<__attribute__((address_space(3))) void*>(dst), 16, off,
-                                             k0, 0, 0);
-  };
-  auto issue = [&](int s) {
-    lds_u8* const base = L + (s & 1) * G::STAGE;
-    const int k0 = s * kTK;
-    if (__builtin_expect(k0 + kTK <= g.K, 1)) {
-#pragma unroll
-      for (int i = 0; i < G::NA; ++i) load(ra, base + (wid * G::NA + i) * 1024, ao[i], k0);
-#pragma unroll
-      for (int i = 0; i < G::NB; ++i) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], k0);
-      return;
-    }
-    // the units past K: zeros in a; what is left of an earlier stage in b
+  auto begin_tile = [&]() {
+    int m0, n0;
+    tile_at(ld_tile, m0, n0);
+    const int rows = int(g.M - m0 < TM ? g.M - m0 : TM), cols = int(g.N - n0 < kTileN ? g.N - n0 : kTileN);
+    ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.a + m0 * g.lda), 0, (rows - 1) * lda + g.K,
+                                           kBufferWord3);
+    rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.b + n0 * g.ldb), 0, (cols - 1) * ldb + g.K,
+                                           kBufferWord3);
 #pragma unroll
     for (int i = 0; i < G::NA; ++i) {
       const int off = (wid * G::NA + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-      if (k0 + 16 * (p ^ swz_x(r)) < g.K) load(ra, base + (wid * G::NA + i) * 1024, ao[i], k0);
-      else *reinterpret_cast<__attribute__((address_space(3))) i32x4*>(base + off) = i32x4{0, 0, 0, 0};
+      ao[i] = uint32_t(min(r, rows - 1)) * lda + 16 * (p ^ swz_x(r));
     }
 #pragma unroll
     for (int i = 0; i < G::NB; ++i) {
       const int off = (wid * G::NB + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-      if (k0 + 16 * (p ^ swz_x(r)) < g.K) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], k0);
+      bo[i] = uint32_t(min(r, cols - 1)) * ldb + 16 * (p ^ swz_x(r));
     }
   };
-  // operands of K-step ks: unit 2 ks + h of rows lr, lr + 32, ...
-  uint32_t unit[4];
+  auto load = [&](__amdgpu_buffer_rsrc_t r, lds_u8* dst, uint32_t off, int k0) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, reinterpret_cast<__attribute__((address_space(3))) void*>(dst), 16, off,
+                                             k0, 0, 0);
+  };
+  auto slot_at = [&](int i) { return L + i * G::STAGE; };
+  auto issue_whole = [&]() {
+    lds_u8* const base = slot_at(ld_slot);
+#pragma unroll
+    for (int i = 0; i < G::NA; ++i) load(ra, base + (wid * G::NA + i) * 1024, ao[i], ld_stage * kTK);
+#pragma unroll
+    for (int i = 0; i < G::NB; ++i) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], ld_stage * kTK);
+    ++ld_stage;
+    ld_slot = ld_slot + 1 == NS ? 0 : ld_slot + 1;
+  };
+  // the next stage of the sequence, if there is one
+  auto issue_next = [&]() {
+    if (ld_tile >= end) return;
+    const int k0 = ld_stage * kTK;
+    if (k0 + kTK <= g.K) {
+      issue_whole();
+    } else {   // the units past K: zeros in a; what is left of an earlier stage in b
+      lds_u8* const base = slot_at(ld_slot);
+#pragma unroll
+      for (int i = 0; i < G::NA; ++i) {
+        const int off = (wid * G::NA + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
+        if (k0 + 16 * (p ^ swz_x(r)) < g.K) load(ra, base + (wid * G::NA + i) * 1024, ao[i], k0);
+        else *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(base + off) = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < G::NB; ++i) {
+        const int off = (wid * G::NB + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
+        if (k0 + 16 * (p ^ swz_x(r)) < g.K) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], k0);
+      }
+      ++ld_stage;
+      ld_slot = ld_slot + 1 == NS ? 0 : ld_slot + 1;
+    }
+    if (ld_stage == stages) {
+      ld_stage = 0;
+      ld_tile += step;
+      if (ld_tile < end) begin_tile();
+    }
+  };
+  // a tile's scales and bias: read into registers, later put into LDS
+  constexpr int kPer = (G::NSC + G::NW * 64 - 1) / (G::NW * 64);
+  float held[kPer];
+  auto fetch_scales = [&](int t) {
+    int m0, n0;
+    tile_at(t, m0, n0);
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int i = tid + u * G::NW * 64, j = i < TM ? i : (i - TM) % kTileN;
+      held[u] = 0.f;
+      if (i < TM) held[u] = m0 + j < g.M ? g.sa[m0 + j] : 0.f;
+      else if (i < G::NSC && n0 + j < g.N) held[u] = i < TM + kTileN ? g.sb[n0 + j] : g.bias ? g.bias[n0 + j] : 0.f;
+    }
+  };
+  auto put_scales = [&](int half) {
+    float* const to = reinterpret_cast<float*>(i8_lds + G::SCALES) + half * G::NSC;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      if (tid + u * G::NW * 64 < G::NSC) to[tid + u * G::NW * 64] = held[u];
+  };
+
+  // ---- products
+  uint32_t unit[4];   // operands of K-step ks: unit 2 ks + h of rows lr, lr + 32, ...
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) unit[ks] = uint32_t(lr) * kTK + 16 * ((2 * ks + h) ^ swz_x(lr));
-  auto read = [&](i32x4(&A)[MI], i32x4(&B)[NI], const lds_u8* base, int ks) {
+  i32x4 A[2][MI], B[2][NI];
+  auto read = [&](int to, const lds_u8* base, int ks) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) A[i] = lds_load<i32x4>(base + unit[ks] + (wm * G::WM + 32 * i) * kTK);
+    for (int i = 0; i < MI; ++i) A[to][i] = lds_load<i32x4>(base + unit[ks] + (wm * G::WM + 32 * i) * kTK);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) B[i] = lds_load<i32x4>(base + G::ABYTES + unit[ks] + (wn * G::WN + 32 * i) * kTK);
+    for (int i = 0; i < NI; ++i)
+      B[to][i] = lds_load<i32x4>(base + G::ABYTES + unit[ks] + (wn * G::WN + 32 * i) * kTK);
   };
-  i32x16 acc[MI][NI] = {};
-  auto multiply = [&](const i32x4(&A)[MI], const i32x4(&B)[NI]) {
+  i32x16 acc[MI][NI];
+  auto multiply = [&](int at) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(B[j], A[i], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NI; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(B[at][j], A[at][i], acc[i][j], 0, 0, 0);
+  };
+  constexpr int kReads = MI + NI, kLoads = G::NA + G::NB;
+  int slot = 0;   // of the stage being computed
+  auto next_slot = [&]() { return slot + 1 == NS ? 0 : slot + 1; };
+  // the steps of a stage but its last
+  auto steps = [&]() {
+    const lds_u8* const base = slot_at(slot);
+    __builtin_amdgcn_sched_barrier(0);
+    read(1, base, 1);
+    multiply(0);
+    spread<kReads, 0, MI * NI>();
+    read(0, base, 2);
+    multiply(1);
+    spread<kReads, 0, MI * NI>();
+    read(1, base, 3);
+    multiply(0);
+    spread<kReads, 0, MI * NI>();
   };
 
-  if (stages > 0) {
-    issue(0);
-    if (stages > 1) issue(1);
-    wait_loads_barrier<0>();
-    i32x4 A[2][MI], B[2][NI];
-    read(A[0], B[0], L, 0);
+  begin_tile();
+#pragma unroll
+  for (int i = 0; i < NS; ++i) issue_next();
+  fetch_scales(cur);
+  put_scales(0);
+  wait_loads_barrier<0>();
+  read(0, slot_at(0), 0);
+  int half = 0;
+  for (; cur < end; cur += step, half ^= 1) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    if (cur + step < end) fetch_scales(cur + step);
+    int s = 0;
+    const int full = stages - 1 - NS;   // stages whose load is of this tile, and not its last: whole
 #pragma unroll 1
-    for (int s = 0; s < stages; ++s) {
-      const lds_u8* const base = L + (s & 1) * G::STAGE;
-      read(A[1], B[1], base, 1);
-      multiply(A[0], B[0]);
-      read(A[0], B[0], base, 2);
-      multiply(A[1], B[1]);
-      read(A[1], B[1], base, 3);
-      multiply(A[0], B[0]);
-      wait_loads_barrier<0>();
-      if (s + 2 < stages) issue(s + 2);
-      if (s + 1 < stages) read(A[0], B[0], L + ((s + 1) & 1) * G::STAGE, 0);
-      multiply(A[1], B[1]);
+    for (; s < full; ++s) {
+      steps();
+      wait_loads_barrier<(NS - 2) * kLoads>();
+      __builtin_amdgcn_sched_barrier(0);
+      issue_whole();
+      slot = next_slot();
+      read(0, slot_at(slot), 0);
+      multiply(1);
+      spread<kReads, kLoads, MI * NI>();
     }
-  }
-  __syncthreads();
+#pragma unroll 1
+    for (; s < stages; ++s) {
+      steps();
+      wait_loads_barrier<0>();
+      issue_next();
+      slot = next_slot();
+      read(0, slot_at(slot), 0);   // (behind the last stage: values that nothing uses)
+      multiply(1);
+    }
+    put_scales(half ^ 1);   // (read in the epilogue before this one, by waves that have met since)
 
-  // Each wave turns 32 tokens at a time through its own part of the LDS: a
-  // lane then holds the same channels of every token, and their scales.
-  float* const buf = reinterpret_cast<float*>(i8_lds) + wid * 32 * G::OUT;
-  constexpr int EB = DT == ARCHEAD_F32 ? 4 : 2, PER = 4, LPR = G::WN / PER;   // lanes to a token's channels
-  const int cc = wn * G::WN + PER * (lane % LPR);
-  float sb[PER], bi[PER];
-  const int cnt = min(max(cols - cc, 0), PER);
+    // ---- outputs: each wave turns 32 tokens x 64 bytes at a time through its
+    // own part of the LDS, so that four lanes store 64 bytes of a token
+    int m0, n0;
+    tile_at(cur, m0, n0);
+    const float* const sc = reinterpret_cast<const float*>(i8_lds + G::SCALES) + half * G::NSC;
+    uint8_t* const buf = i8_lds + G::OUT + wid * 32 * G::OROW;
+    constexpr int EB = DT == ARCHEAD_F32 ? 4 : 2, PER = 16 / EB;   // elements of 16 bytes
+    const bool whole = m0 + TM <= g.M && n0 + kTileN <= g.N;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    sb[i] = i < cnt ? g.sb[n0 + cc + i] : 0.f;
-    bi[i] = g.bias && i < cnt ? g.bias[n0 + cc + i] : 0.f;
-  }
+    for (int mi = 0; mi < MI; ++mi) {
+      const float sa = sc[wm * G::WM + 32 * mi + lr];
+      const int64_t r0 = m0 + wm * G::WM + 32 * mi;
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi) {
+      for (int ni = 0; ni < NI; ++ni) {
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
+        for (int part = 0; part < EB / 2; ++part) {   // 16 or 32 channels
+          constexpr int KP = 8 / EB;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<f32x4*>(buf + lr * G::OUT + 32 * ni + 8 * k + 4 * h) =
-            f32x4{float(acc[mi][ni][4 * k]), float(acc[mi][ni][4 * k + 1]), float(acc[mi][ni][4 * k + 2]),
-                  float(acc[mi][ni][4 * k + 3])};
-    const int r0 = wm * G::WM + 32 * mi;
+          for (int kk = 0; kk < KP; ++kk) {
+            const int k = part * KP + kk, c = wn * G::WN + 32 * ni + 8 * k + 4 * h;
+            const f32x4 sb = *reinterpret_cast<const f32x4*>(sc + TM + c);
+            const f32x4 bi = *reinterpret_cast<const f32x4*>(sc + TM + kTileN + c);
+            float y[4];
 #pragma unroll
-    for (int j = 0; j < 32 * LPR / 64; ++j) {
-      const int rl = j * (64 / LPR) + lane / LPR;
-      const f32x4 v = *reinterpret_cast<const f32x4*>(buf + rl * G::OUT + PER * (lane % LPR));
-      if (r0 + rl >= rows || cnt == 0) continue;
-      const float sa = g.sa[m0 + r0 + rl];
-      float y[PER];
+            for (int i = 0; i < 4; ++i) y[i] = scaled(acc[mi][ni][4 * k + i], sa, sb[i], bi[i], g.bias != nullptr);
+            put4<DT>(buf + lr * G::OROW + (8 * kk + 4 * h) * EB, y);
+          }
+          wave_lds_order();
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        y[i] = v[i] * sa * sb[i];
-        if (g.bias) y[i] += bi[i];
+          for (int j = 0; j < 2; ++j) {
+            const int rl = 16 * j + lane / 4, q = lane & 3;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(buf + rl * G::OROW + 16 * q);
+            const int64_t n = n0 + wn * G::WN + 32 * ni + (32 / (EB / 2)) * part + q * PER;
+            uint8_t* const p = g.out + ((r0 + rl) * g.ldo + n) * EB;
+            if (whole) {
+              store_any(p, v);
+            } else if (r0 + rl < g.M) {
+              store_part<EB>(p, v, g.N - n);
+            }
+          }
+          wave_lds_order();
+        }
       }
-      store4<DT>(g.out + ((m0 + r0 + rl) * g.ldo + n0 + cc) * EB, y, cnt);
     }
   }
 }
 
-template <int DT, int TM, int WMW, int WNW>
-void launch(const I8Args& g, hipStream_t s) {
-  using G = Geom<TM, WMW, WNW>;
-  const int64_t mt = (g.M + TM - 1) / TM, nt = (g.N + kTileN - 1) / kTileN, per = (mt * nt + 7) / 8;
-  const void* fn = reinterpret_cast<const void*>(k_i8_tile<DT, TM, WMW, WNW>);
-  int m_tiles = int(mt), n_tiles = int(nt);
-  int64_t per_xcd = per;
-  void* args[] = {const_cast<I8Args*>(&g), &m_tiles, &n_tiles, &per_xcd};
+template <int DT, int TM, int WMW, int WNW, int NS>
+void launch(const I8Args& g, int n_cu, hipStream_t s) {
+  using G = Geom<TM, WMW, WNW, NS>;
+  int m_tiles = int((g.M + TM - 1) / TM), n_tiles = int((g.N + kTileN - 1) / kTileN);
+  int per_xcd = (m_tiles * n_tiles + 7) / 8;
+  const void* fn = reinterpret_cast<const void*>(k_i8_tile<DT, TM, WMW, WNW, NS>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS) != hipSuccess) return;
-  (void)hipLaunchKernel(fn, dim3(unsigned(8 * per)), dim3(G::NW * 64), args, G::LDS, s);
+  const int wgs = 8 * std::min(per_xcd, std::max(n_cu / 8, 1));
+  void* args[] = {const_cast<I8Args*>(&g), &m_tiles, &n_tiles, &per_xcd};
+  (void)hipLaunchKernel(fn, dim3(unsigned(wgs)), dim3(G::NW * 64), args, G::LDS, s);
 }
 
 }  // namespace
@@ -199,18 +322,21 @@ namespace archead {
 namespace i8 {
 
 bool tiles_take(const I8Args& g) {
-  const int64_t tiles = ((g.M + 255) / 256) * ((g.N + kTileN - 1) / kTileN);
+  const int64_t tiles = ((g.M + 63) / 64) * ((g.N + kTileN - 1) / kTileN);
   return aligned(g.a, 16) && aligned(g.b, 16) && g.K % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.K > 0 &&
          g.lda <= kMaxLd && g.ldb <= kMaxLd && tiles < (1 << 22) && g.M > 64;
 }
 
+#ifndef I8TM
+#define I8TM 256, 2, 4, 2
+#endif
 template <int DT>
-void launch_tiles(const I8Args& g, hipStream_t s) {
-  launch<DT, 256, 2, 4>(g, s);
+void launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
+  launch<DT, I8TM>(g, n_cu, s);
 }
-template void launch_tiles<ARCHEAD_F32>(const I8Args&, hipStream_t);
-template void launch_tiles<ARCHEAD_BF16>(const I8Args&, hipStream_t);
-template void launch_tiles<ARCHEAD_F16>(const I8Args&, hipStream_t);
+template void launch_tiles<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
+template void launch_tiles<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
+template void launch_tiles<ARCHEAD_F16>(const I8Args&, int, hipStream_t);
 
 }  // namespace i8
 }  // namespace archead

@@ -1,5 +1,7 @@
 // archead_matmul_i8: products of 8-bit integers with a scale per row of each
 // operand.
+#include <atomic>
+
 #include "i8.cuh"
 
 namespace {
@@ -68,9 +70,22 @@ __global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, i
   }
 }
 
+// compute units of the current device, asked for once
+int compute_units() {
+  static std::atomic<int> known[64];
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 256;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 template <int DT>
 void launch_matmul(const I8Args& g, hipStream_t s) {
-  if (tiles_take(g)) return launch_tiles<DT>(g, s);
+  if (tiles_take(g)) return launch_tiles<DT>(g, compute_units(), s);
   const int64_t mt = (g.M + kATile - 1) / kATile, nt = (g.N + kATile - 1) / kATile, tiles = mt * nt;
   const dim3 grid{unsigned(tiles < (1 << 22) ? tiles : 1 << 22)};
   hipLaunchKernelGGL(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
