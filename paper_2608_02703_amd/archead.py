@@ -201,7 +201,8 @@ def _load(path: str, names) -> ctypes.CDLL:
 def lib() -> ctypes.CDLL:
     """The HIP library (all entry points).  ARCHEAD_LIB may name another
     build of it (tuning experiments)."""
-    return _load(os.environ.get("ARCHEAD_LIB", LIB_PATH), list(_SIGS))
+    path = os.environ.get("ARCHEAD_LIB", LIB_PATH)
+    return _libs.get(path) or _load(path, _SIGS)
 
 
 def host_lib(path: Optional[str] = None) -> ctypes.CDLL:
@@ -298,46 +299,60 @@ def logit_fidelity(ref, test):
     return kl, sq, idx, rank
 
 
+_FLOAT_CODES = {}   # torch dtype -> dtype code, filled when torch is there
+
+
 def _float_code(dtype, what):
-    import torch
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(dtype)
+    if not _FLOAT_CODES:
+        import torch
+        _FLOAT_CODES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    code = _FLOAT_CODES.get(dtype)
     if code is None:
         raise TypeError(f"{what} must be float32, bfloat16 or float16")
     return code
 
 
-def _matrix(t, what, device, dtype=None, shape=None):
-    """The leading dimension of a 2-D tensor on `device` with unit column
-    stride (of a single row, one that holds the row)."""
-    if t.device != device or t.device.type != "cuda":
-        raise ValueError(f"{what} must be on {device if device.type == 'cuda' else 'a GPU'}")
+def _gpu_of(t, what):
+    """Index of the GPU a tensor is on."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be on a GPU")
+    return t.get_device()
+
+
+def _matrix(t, what, gpu, dtype=None, shape=None):
+    """The leading dimension of a 2-D tensor on a GPU with unit column stride
+    (of a single row, one that holds the row)."""
+    if t.get_device() != gpu or not t.is_cuda:
+        raise ValueError(f"{what} must be on GPU {gpu}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError(f"{what} must be 2-D" if shape is None else f"{what} must have shape {list(shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{what} must have unit column stride")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return ld if rows > 1 else max(ld, cols)
 
 
-def _dense(t, what, device, dtypes, shape):
-    """Checks a contiguous tensor of a shape and one of some dtypes on `device`."""
-    if t.device != device:
-        raise ValueError(f"{what} must be on {device}")
+def _dense(t, what, gpu, dtypes, shape):
+    """Checks a contiguous tensor of a shape and one of some dtypes on a GPU."""
+    if t.get_device() != gpu or not t.is_cuda:
+        raise ValueError(f"{what} must be on GPU {gpu}")
     if t.dtype not in dtypes:
         raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}")
-    if tuple(t.shape) != shape or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous with shape {list(shape)}")
 
 
-def _launch(device, fn, *args):
-    """fn(*args, stream) with `device` the current one, on its current stream."""
+def _launch(gpu, fn, *args):
+    """fn(*args, stream) with `gpu` the current one, on its current stream (its
+    handle without a Stream object: these calls take a few microseconds)."""
     import torch
-    if torch.cuda.current_device() == device.index:
-        st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if torch.cuda.current_device() == gpu:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(gpu):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
     if st != OK:
         _check(st)
 
@@ -348,18 +363,20 @@ def quantize_i8(x, codes=None, scales=None):
     scales[:, None] (archead_quantize_i8).  Rows are tokens, or the output
     channels of a weight."""
     import torch
-    dev = x.device
-    ldx = _matrix(x, "x", dev)
+    gpu = _gpu_of(x, "x")
+    ldx = _matrix(x, "x", gpu)
     code = _float_code(x.dtype, "x")
     M, d = x.shape
+    ldc = d
     if codes is None:
-        codes = torch.empty((M, d), dtype=torch.int8, device=dev)
-    ldc = _matrix(codes, "codes", dev, torch.int8, (M, d))
-    if scales is None:
-        scales = torch.empty(M, dtype=torch.float32, device=dev)
+        codes = torch.empty((M, d), dtype=torch.int8, device=x.device)
     else:
-        _dense(scales, "scales", dev, (torch.float32,), (M,))
-    _launch(dev, lib().archead_quantize_i8, x.data_ptr(), code, M, d, ldx, codes.data_ptr(), ldc,
+        ldc = _matrix(codes, "codes", gpu, torch.int8, (M, d))
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device=x.device)
+    else:
+        _dense(scales, "scales", gpu, (torch.float32,), (M,))
+    _launch(gpu, lib().archead_quantize_i8, x.data_ptr(), code, M, d, ldx, codes.data_ptr(), ldc,
             scales.data_ptr())
     return codes, scales
 
@@ -370,51 +387,53 @@ def matmul_i8(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=None):
     Scales and bias are float32; out is float32 (the default), bfloat16 or
     float16."""
     import torch
-    dev = a.device
-    lda = _matrix(a, "a", dev, torch.int8)
-    ldb = _matrix(b, "b", dev, torch.int8)
+    gpu = _gpu_of(a, "a")
+    lda = _matrix(a, "a", gpu, torch.int8)
+    ldb = _matrix(b, "b", gpu, torch.int8)
     M, K = a.shape
-    N = b.shape[0]
-    if b.shape[1] != K:
+    N, Kb = b.shape
+    if Kb != K:
         raise ValueError("a and b must have the same number of columns")
-    _dense(a_scales, "a_scales", dev, (torch.float32,), (M,))
-    _dense(b_scales, "b_scales", dev, (torch.float32,), (N,))
+    f32 = (torch.float32,)
+    _dense(a_scales, "a_scales", gpu, f32, (M,))
+    _dense(b_scales, "b_scales", gpu, f32, (N,))
     if bias is not None:
-        _dense(bias, "bias", dev, (torch.float32,), (N,))
+        _dense(bias, "bias", gpu, f32, (N,))
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype or torch.float32, device=dev)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError("out and out_dtype disagree")
-    ldo = _matrix(out, "out", dev, None, (M, N))
-    _launch(dev, lib().archead_matmul_i8, a.data_ptr(), lda, a_scales.data_ptr(), b.data_ptr(), ldb,
-            b_scales.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(),
-            _float_code(out.dtype, "out"), ldo)
+        out_dtype = out_dtype or torch.float32
+        code = _float_code(out_dtype, "out_dtype")
+        out, ldo = torch.empty((M, N), dtype=out_dtype, device=a.device), N
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError("out and out_dtype disagree")
+        code = _float_code(out.dtype, "out")
+        ldo = _matrix(out, "out", gpu, None, (M, N))
+    _launch(gpu, lib().archead_matmul_i8, a.data_ptr(), lda, a_scales.data_ptr(), b.data_ptr(), ldb,
+            b_scales.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), code, ldo)
     return out
 
 
-def _beam_call(dev, V, scores, n, finished, end_token, ws, ws_bytes, call):
+def _beam_call(gpu, device, scores, n, finished, end_token, ws, ws_bytes, call):
     """Outputs and workspace of a beam selection, around call(...)."""
     import torch
     if scores.dim() != 2:
         raise ValueError("scores must be [B, K]")
     B, K = scores.shape
-    _dense(scores, "scores", dev, (torch.float32,), (B, K))
+    _dense(scores, "scores", gpu, (torch.float32,), (B, K))
     if finished is not None:
-        _dense(finished, "finished", dev, (torch.bool, torch.uint8), (B, K))
+        _dense(finished, "finished", gpu, (torch.bool, torch.uint8), (B, K))
     n = int(n)
     if not 1 <= n <= TOPK_MAX:
         raise ValueError(f"n must be in 1 .. {TOPK_MAX}")
-    out = torch.empty((B, n), dtype=torch.float32, device=dev)
-    pair = torch.empty((2, B, n), dtype=torch.int64, device=dev)
-    parents, tokens = pair[0], pair[1]
-    ended = torch.empty((B, n), dtype=torch.bool, device=dev) if end_token >= 0 else None
-    need = ws_bytes(B * K)
+    out = torch.empty((B, n), dtype=torch.float32, device=device)
+    parents, tokens = torch.empty((2, B, n), dtype=torch.int64, device=device).unbind(0)
+    ended = torch.empty((B, n), dtype=torch.bool, device=device) if end_token >= 0 else None
     if ws is None:
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-    elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous uint8 tensor on the same device")
-    call(B, K, _ptr(scores), _ptr(finished), int(end_token), n, _ptr(out), _ptr(parents), _ptr(tokens),
-         _ptr(ended), _ptr(ws), ws.numel())
+        ws = torch.empty(max(ws_bytes(B * K), 256), dtype=torch.uint8, device=device)
+    elif ws.get_device() != gpu or not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous uint8 tensor on the same GPU")
+    call(B, K, scores.data_ptr(), _ptr(finished), int(end_token), n, out.data_ptr(), parents.data_ptr(),
+         tokens.data_ptr(), _ptr(ended), ws.data_ptr(), ws.numel())
     return (out, parents, tokens) if ended is None else (out, parents, tokens, ended)
 
 
@@ -427,8 +446,8 @@ def beam_select(logits, scores, n, finished=None, end_token=-1, ws=None):
     Returns (scores float32 [B, n], parents int64 [B, n], tokens int64 [B,
     n]), best first, and with an end_token also which of them have ended, bool
     [B, n].  Empty places hold (-inf, -1, -1)."""
-    dev = logits.device
-    ldl = _matrix(logits, "logits", dev)
+    gpu = _gpu_of(logits, "logits")
+    ldl = _matrix(logits, "logits", gpu)
     code = _float_code(logits.dtype, "logits")
     R, V = logits.shape
     if scores.numel() != R:
@@ -436,8 +455,8 @@ def beam_select(logits, scores, n, finished=None, end_token=-1, ws=None):
     L = lib()
 
     def call(B, K, *rest):
-        _launch(dev, L.archead_beam_select, logits.data_ptr(), code, B, K, V, ldl, *rest)
-    return _beam_call(dev, V, scores, n, finished, end_token, ws,
+        _launch(gpu, L.archead_beam_select, logits.data_ptr(), code, B, K, V, ldl, *rest)
+    return _beam_call(gpu, logits.device, scores, n, finished, end_token, ws,
                       lambda rows: L.archead_beam_workspace_bytes(rows, V), call)
 
 
@@ -469,9 +488,9 @@ class BeamStates:
         self.batch = self.device = None
         groups = {}
         for i, (s, d) in enumerate(zip(states, self.out)):
-            if s.device.type != "cuda" or d.device != s.device or (self.device or s.device) != s.device:
+            if not s.is_cuda or d.device != s.device or (self.device or s.device) != s.device:
                 raise ValueError("states and out must be on one GPU")
-            self.device = s.device
+            self.device, self._gpu = s.device, s.get_device()
             if s.dim() == 0 or not -s.dim() <= row_dim < s.dim():
                 raise ValueError("states must have a dimension row_dim")
             r = row_dim % s.dim()
@@ -548,15 +567,15 @@ class BeamStates:
         if not self._groups:
             return self.out
         B, n = self.batch, self.out_beams
-        _dense(parents, "parents", self.device, (torch.int64, torch.int32), (B, n))
+        _dense(parents, "parents", self._gpu, (torch.int64, torch.int32), (B, n))
         if lengths is not None:
             if not self.has_pos:
                 raise ValueError("lengths need pos_dim")
-            _dense(lengths, "lengths", self.device, (torch.int32,), (B,))
+            _dense(lengths, "lengths", self._gpu, (torch.int32,), (B,))
         idx = I64 if parents.dtype == torch.int64 else I32
         fn = lib().archead_beam_reorder
         for layout, count, src, dst in self._groups:
-            _launch(self.device, fn, layout, count, src, dst, B, self.beams, n, parents.data_ptr(), idx,
+            _launch(self._gpu, fn, layout, count, src, dst, B, self.beams, n, parents.data_ptr(), idx,
                     _ptr(lengths))
         return self.out
 
@@ -837,14 +856,14 @@ class PackedHead:
         """beam_select over this head's logits of the beams' hidden states x,
         bf16 [B * K, d] (archead_logits_beam)."""
         import torch
-        dev = x.device
-        ldx = _matrix(x, "x", dev, torch.bfloat16)
+        gpu = _gpu_of(x, "x")
+        ldx = _matrix(x, "x", gpu, torch.bfloat16)
         if x.shape[1] != self.d or scores.numel() != x.shape[0]:
             raise ValueError("x must have d columns and a row for every beam of scores")
 
         def call(B, K, *rest):
-            _launch(dev, self._lib.archead_logits_beam, self.handle, x.data_ptr(), B, K, ldx, *rest)
-        return _beam_call(dev, self.V, scores, n, finished, end_token, ws,
+            _launch(gpu, self._lib.archead_logits_beam, self.handle, x.data_ptr(), B, K, ldx, *rest)
+        return _beam_call(gpu, x.device, scores, n, finished, end_token, ws,
                           lambda rows: self.workspace_bytes(rows, OP_BEAM), call)
 
     def logit_fidelity_head(self, x, dense, ws=None):

@@ -2,6 +2,9 @@
 #include "dev_common.cuh"
 #include "i8.cuh"
 
+#ifndef I8MIN
+#define I8MIN 64
+#endif
 namespace {
 
 using namespace archead::i8;
@@ -324,7 +327,7 @@ namespace i8 {
 bool tiles_take(const I8Args& g) {
   const int64_t tiles = ((g.M + 63) / 64) * ((g.N + kTileN - 1) / kTileN);
   return aligned(g.a, 16) && aligned(g.b, 16) && g.K % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.K > 0 &&
-         g.lda <= kMaxLd && g.ldb <= kMaxLd && tiles < (1 << 22) && g.M > 64;
+         g.lda <= kMaxLd && g.ldb <= kMaxLd && tiles < (1 << 22) && g.M > I8MIN;
 }
 
 #ifndef I8TM

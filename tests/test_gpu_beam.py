@@ -432,6 +432,27 @@ def test_reorder_many_states_and_graph():
         assert all(torch.equal(s.cpu(), t) for s, t in zip(states, ref))
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_reorder_beyond_the_caches(in_place):
+    """More bytes than the caches hold (another kind of stores)."""
+    from paper_2608_02703_amd import BeamStates
+    B, K, T = 2, 3, 1001
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    states = [torch.randint(0, 99, (B * K, 8, T, 4096), generator=gen, device="cuda", dtype=torch.int8)
+              for _ in range(2)]
+    out = None if in_place else [torch.full_like(s, 7) for s in states]
+    p = torch.tensor([[2, 0, 2], [1, 2, 0]], device="cuda")
+    lengths = torch.tensor([T, 650], dtype=torch.int32, device="cuda")
+    old = [s.clone() for s in states]
+    for s, g in zip(old, BeamStates(states, K, out, pos_dim=2).reorder(p, lengths)):
+        for b in range(B):
+            n = int(lengths[b])
+            for j in range(K):
+                assert torch.equal(g[b * K + j, :, :n], s[b * K + int(p[b, j]), :, :n])
+                rest = s[b * K + j, :, n:]
+                assert torch.equal(g[b * K + j, :, n:], rest if in_place else torch.full_like(rest, 7))
+
+
 def test_reorder_far_rows():
     """Rows whose offsets pass 32 bits."""
     from paper_2608_02703_amd import BeamStates
