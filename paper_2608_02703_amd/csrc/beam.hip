@@ -41,13 +41,55 @@ struct ScanArgs {
   archead::BeamSpanSum* span;   // [rows][n_span]
 };
 
+// The best of the lanes' values, in every lane: within rows of 16 lanes without
+// LDS, then across the four rows.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float lane_f(float v, int l) {
+  return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), l)));
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float v) {
+  return __uint_as_float(dpp_u<CTRL>(__float_as_uint(v)));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  v = fmaxf(v, dpp_f<0x140>(v));
+  return fmaxf(fmaxf(lane_f(v, 0), lane_f(v, 16)), fmaxf(lane_f(v, 32), lane_f(v, 48)));
+}
+__device__ __forceinline__ double of_words(uint32_t lo, uint32_t hi) {
+  return __longlong_as_double((long long)(uint64_t(hi) << 32 | lo));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = uint64_t(__double_as_longlong(v));
+  return of_words(dpp_u<CTRL>(uint32_t(u)), dpp_u<CTRL>(uint32_t(u >> 32)));
+}
+__device__ __forceinline__ double lane_d(double v, int l) {
+  const uint64_t u = uint64_t(__double_as_longlong(v));
+  return of_words(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(u)), l)),
+                  uint32_t(__builtin_amdgcn_readlane(int(uint32_t(u >> 32)), l)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  v += dpp_d<0x140>(v);
+  return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
+}
+
+// a wave to a span: its chunks' largest logits, its sum of exponentials
 template <int DT>
 __global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
   const int lane = threadIdx.x & 63;
   const int wid = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int64_t r = blockIdx.y, sp = int64_t(blockIdx.x) * (kScanBlock / 64) + wid;
   if (sp >= a.n_span) return;
-  if (!(fabsf(a.scores[r]) < INFINITY) || (a.finished && a.finished[r])) return;   // offers nothing by its logits
+  if (!(fabsf(a.scores[r]) < INFINITY) || (a.finished && a.finished[r])) return;   // its logits say nothing
   const uint8_t* row = a.logits + r * a.row_bytes;
   Eight<DT> e[kSpanChunks];
 #pragma unroll
@@ -59,10 +101,8 @@ __global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
     float m = e[c].at(0);
 #pragma unroll
     for (int i = 1; i < 8; ++i) m = fmaxf(m, e[c].at(i));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    cm[c] = m;
-    top = fmaxf(top, m);
+    cm[c] = wave_max(m);
+    top = fmaxf(top, cm[c]);
   }
   // relative to 0 where nothing is above -inf: every term is then 0, or NaN
   const float ref = top > -INFINITY ? top : 0.f;
@@ -71,19 +111,22 @@ __global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
   for (int c = 0; c < kSpanChunks; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f((e[c].at(i) - ref) * 1.4426950408889634f);
-  double sd = s;
+  const double sd = wave_sum(double(s));
+  if (lane == 0) a.span[r * a.n_span + sp] = archead::BeamSpanSum{sd, ref};
+  if (lane < kSpanChunks) {
+    float m = cm[0];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sd += __shfl_xor(sd, o, 64);
-  if (lane == 0) {
-    a.span[r * a.n_span + sp] = archead::BeamSpanSum{sd, ref};
-#pragma unroll
-    for (int c = 0; c < kSpanChunks; ++c) a.cmax[(r * a.n_span + sp) * kSpanChunks + c] = cm[c];
+    for (int c = 1; c < kSpanChunks; ++c) m = lane == c ? cm[c] : m;
+    a.cmax[(r * a.n_span + sp) * kSpanChunks + lane] = m;
   }
 }
-
 constexpr int kPickBlock = 1024, kPickWaves = kPickBlock / 64;
+constexpr int kPickHeld = 4;     // chunks whose largest logits a thread keeps
+constexpr int kPickSpans = 4;    // spans whose sums a lane keeps
+constexpr int kPickGroups = kPickBlock / 16;   // groups of threads that share a maximum
 constexpr int kPickList = 512;   // chunks, and pairs, that are ranked one against all
 static_assert(kPickList >= archead::kTopKMaxK + ARCHEAD_BEAM_MAX, "room for the n best and the ended beams");
+static_assert(kPickGroups == 64, "a lane of a wave for each");
 
 struct PickArgs {
   ScanArgs in;
@@ -94,8 +137,12 @@ struct PickArgs {
   uint8_t* out_finished;   // may be null
 };
 
-// the order of pairs (position k * V + v) and of chunks (their number)
-__device__ __forceinline__ bool before(double sa, int64_t ia, double sb, int64_t ib) {
+struct __align__(16) Ranked {
+  double score;
+  uint64_t at;
+};
+// the order of pairs (beam << 32 | token) and of chunks (their number)
+__device__ __forceinline__ bool before(double sa, uint64_t ia, double sb, uint64_t ib) {
   return sa > sb || (sa == sb && ia < ib);
 }
 
@@ -103,86 +150,114 @@ template <int DT>
 __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   __shared__ double lse[ARCHEAD_BEAM_MAX], cum[ARCHEAD_BEAM_MAX];   // lse: NaN where a row offers nothing by its logits
   __shared__ bool ended[ARCHEAD_BEAM_MAX];
-  __shared__ uint32_t skey[kPickBlock];
-  __shared__ double lscore[kPickList];
-  __shared__ int64_t lat[kPickList];
+  __shared__ uint32_t skey[kPickGroups];
+  __shared__ Ranked list[kPickList];
   __shared__ int chunks[kPickList];
   __shared__ double wscore[kPickWaves];
-  __shared__ int64_t wat[kPickWaves];
+  __shared__ uint64_t wat[kPickWaves];
   __shared__ int n_list, n_pair;
-  __shared__ uint32_t sfloor;
   const ScanArgs& a = p.in;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t b = blockIdx.x, r0 = b * p.K;
-  const int n_chunk = int(a.n_span) * kSpanChunks, n_items = n_chunk * p.K;   // (K V / 512 < 2^27)
+  const int n_span = int(a.n_span), n_chunk = n_span * kSpanChunks, n_items = n_chunk * p.K;   // (K V / 512 < 2^27)
   if (tid == 0) n_list = n_pair = 0;
+  // item i of u: chunk i % n_chunk of beam i / n_chunk; neighbouring items go
+  // to different groups of 16 threads
+  auto item_at = [&](int u) { return u * kPickBlock + (tid & 15) * kPickGroups + (tid >> 4); };
+  float held[kPickHeld];   // (of rows that say nothing: whatever the workspace holds)
+#pragma unroll
+  for (int u = 0; u < kPickHeld; ++u) held[u] = item_at(u) < n_items ? a.cmax[r0 * n_chunk + item_at(u)] : -INFINITY;
   for (int k = wid; k < p.K; k += kPickWaves) {
-    const double c = a.scores[r0 + k];
-    const bool f = a.finished && a.finished[r0 + k], alive = fabs(c) < INFINITY && !f;
-    double m = -INFINITY, s = 0.0;
-    if (alive) {
-      const archead::BeamSpanSum* sp = a.span + (r0 + k) * a.n_span;
+    const archead::BeamSpanSum* const sp = a.span + (r0 + k) * a.n_span;
+    archead::BeamSpanSum first[kPickSpans];
+#pragma unroll
+    for (int u = 0; u < kPickSpans; ++u)
+      first[u] = lane + 64 * u < n_span ? sp[lane + 64 * u] : archead::BeamSpanSum{0.0, 0.f};
+    const float c = a.scores[r0 + k];
+    const bool f = a.finished && a.finished[r0 + k];
+    double l = NAN;
+    if (fabsf(c) < INFINITY && !f) {
       // (a span with nothing above -inf has the sum 0, whatever its maximum)
-      for (int64_t i = lane; i < a.n_span; i += 64)
-        if (sp[i].sum != 0.0) m = fmax(m, double(sp[i].top));
+      float top = -INFINITY;
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) m = fmax(m, __shfl_xor(m, o, 64));
-      for (int64_t i = lane; i < a.n_span; i += 64)
-        if (sp[i].sum != 0.0) s += sp[i].sum * exp(double(sp[i].top) - m);
+      for (int u = 0; u < kPickSpans; ++u) top = first[u].sum != 0.0 ? fmaxf(top, first[u].top) : top;
+      for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) top = sp[i].sum != 0.0 ? fmaxf(top, sp[i].top) : top;
+      top = wave_max(top);
+      double s = 0.0;
+      auto add = [&](const archead::BeamSpanSum& v) {
+        if (v.sum != 0.0) s += v.sum * exp(double(v.top) - double(top));
+      };
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+      for (int u = 0; u < kPickSpans; ++u) add(first[u]);
+      for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) add(sp[i]);
+      s = wave_sum(s);
+      // +inf among the logits: a term inf - inf, so the sum is NaN
+      if (s > 0.0) l = top + log(s);
     }
     if (lane == 0) {
-      // +inf among the logits: a term inf - inf, so the sum is NaN
-      lse[k] = alive && s > 0.0 ? m + log(s) : double(NAN);
+      lse[k] = l;
       cum[k] = c;
       ended[k] = f;
     }
   }
   __syncthreads();
   auto score_of = [&](int k, float logit) { return cum[k] + (double(logit) - lse[k]); };
-  auto chunk_score = [&](int item) {
+  auto chunk_score = [&](int item, float top) {
     const int k = item / n_chunk;
-    return lse[k] == lse[k] ? score_of(k, a.cmax[r0 * n_chunk + item]) : double(-INFINITY);
+    return lse[k] == lse[k] ? score_of(k, top) : double(-INFINITY);
   };
-  // ---- a floor: the n-th largest of the threads' best chunks (the order's
-  // first 32 bits)
+  auto score_again = [&](int item) { return chunk_score(item, a.cmax[r0 * n_chunk + item]); };
+  // ---- a floor: about the n-th largest of the groups' best chunks, in the
+  // order's first 32 bits
+  double mine[kPickHeld];
   uint32_t best = 0;
-  for (int i = tid; i < n_items; i += kPickBlock) best = max(best, uint32_t(order_key(chunk_score(i)) >> 32));
-  skey[tid] = best;
-  __syncthreads();
-  if (wid == 0) {
-    uint32_t kk[kPickWaves];
 #pragma unroll
-    for (int i = 0; i < kPickWaves; ++i) kk[i] = skey[64 * i + lane];
-    uint32_t f = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t t = f | (1u << bit);
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < kPickWaves; ++i) c += __popcll(__ballot(kk[i] >= t));
-      f = c >= p.n ? t : f;
-    }
-    if (lane == 0) sfloor = max(f, 1u);   // 1: every candidate
+  for (int u = 0; u < kPickHeld; ++u) {
+    mine[u] = item_at(u) < n_items ? chunk_score(item_at(u), held[u]) : -INFINITY;
+    best = max(best, uint32_t(order_key(mine[u]) >> 32));
   }
+  for (int u = kPickHeld; u * kPickBlock < n_items; ++u)
+    if (item_at(u) < n_items) best = max(best, uint32_t(order_key(score_again(item_at(u))) >> 32));
+  best = max(best, dpp_u<0xB1>(best));
+  best = max(best, dpp_u<0x4E>(best));
+  best = max(best, dpp_u<0x141>(best));
+  best = max(best, dpp_u<0x140>(best));
+  if ((tid & 15) == 0) skey[tid >> 4] = best;
   __syncthreads();
-  const uint32_t floor = sfloor;
+  // (every wave finds it: no second meeting)
+  uint32_t floor = 0;
+  {
+    const uint32_t key = skey[lane];
+    int reach = kPickGroups;
+    const int enough = p.n + p.n / 4;
+    for (int bit = 31; bit >= 0 && reach > enough; --bit) {
+      const uint32_t t = floor | (1u << bit);
+      const int c = __popcll(__ballot(key >= t));
+      if (c >= p.n) {
+        floor = t;
+        reach = c;
+      }
+    }
+    floor = max(floor, 1u);   // 1: every candidate
+  }
   // ---- the chunks that reach it
-  for (int i = tid; i < n_items; i += kPickBlock) {
-    const double s = chunk_score(i);
-    if (uint32_t(order_key(s) >> 32) >= floor) {
-      const int at = atomicAdd(&n_list, 1);
-      if (at < kPickList) chunks[at] = i;
-    }
-  }
+  auto list_chunk = [&](int i, double s) {
+    if (uint32_t(order_key(s) >> 32) < floor) return;
+    const int at = atomicAdd(&n_list, 1);
+    if (at < kPickList) chunks[at] = i;
+  };
+#pragma unroll
+  for (int u = 0; u < kPickHeld; ++u) list_chunk(item_at(u), mine[u]);
+  for (int u = kPickHeld; u * kPickBlock < n_items; ++u)
+    if (item_at(u) < n_items) list_chunk(item_at(u), score_again(item_at(u)));
   __syncthreads();
-  // The best of the threads' (s, i), in every thread.
-  auto workgroup_best = [&](double& s, int64_t& i) {
+  // the best of the threads' (s, i), in every thread
+  auto workgroup_best = [&](double& s, uint64_t& i) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       const double os = __shfl_xor(s, o, 64);
-      const int64_t oi = __shfl_xor((long long)i, o, 64);
+      const uint64_t oi = __shfl_xor((unsigned long long)i, o, 64);
       if (before(os, oi, s, i)) {
         s = os;
         i = oi;
@@ -207,13 +282,13 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   if (__builtin_expect(n_ch > kPickList, 0)) {
     // many that are equal or nearly so: the first n of the ranking, one a round
     double as = INFINITY;
-    int64_t ai = -1;
+    uint64_t ai = 0;
     n_ch = 0;
     for (int j = 0; j < p.n; ++j) {
       double s = -INFINITY;
-      int64_t at = INT64_MAX;
+      uint64_t at = UINT64_MAX;
       for (int i = tid; i < n_items; i += kPickBlock) {
-        const double si = chunk_score(i);
+        const double si = score_again(i);
         if (si > -INFINITY && before(as, ai, si, i) && before(si, i, s, at)) {
           s = si;
           at = i;
@@ -229,37 +304,42 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     __syncthreads();
   }
   // ---- the pairs at or above the floor, and the ended beams'
-  auto token_at = [&](int item, int i) {   // of element i of this lane in a chunk
-    return int64_t(item % n_chunk) * archead::kBeamChunk + lane * 8 + i;
-  };
-  if (tid < p.K && ended[tid] && fabs(cum[tid]) < INFINITY) {
-    const int at = atomicAdd(&n_pair, 1);
-    if (at < kPickList) {
-      lscore[at] = cum[tid];
-      lat[at] = tid * a.V + p.end_token;
-    }
-  }
-  for (int c = wid; c < n_ch; c += kPickWaves) {
+  auto offers_end = [&](int k) { return k < p.K && ended[k] && fabs(cum[k]) < INFINITY; };
+  auto pair = [&](int k, int64_t v) { return uint64_t(k) << 32 | uint64_t(v); };
+  auto fetch = [&](Eight<DT>& e, int c) {   // this lane's eight logits of listed chunk c
     const int item = chunks[c], k = item / n_chunk;
-    Eight<DT> e;
-    e.load(a.logits + (r0 + k) * a.row_bytes, token_at(item, 0), a.V, neg_inf<DT>());
+    e.load(a.logits + (r0 + k) * a.row_bytes, int64_t(item - k * n_chunk) * archead::kBeamChunk + lane * 8, a.V,
+           neg_inf<DT>());
+  };
+  auto each = [&](const Eight<DT>& e, int c, auto use) {   // use(score, pair) for them
+    const int item = chunks[c], k = item / n_chunk;
+    const int64_t v0 = int64_t(item - k * n_chunk) * archead::kBeamChunk + lane * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const double s = score_of(k, e.at(i));
-      if (uint32_t(order_key(s) >> 32) >= floor) {
-        const int at = atomicAdd(&n_pair, 1);
-        if (at < kPickList) {
-          lscore[at] = s;
-          lat[at] = k * a.V + token_at(item, i);
-        }
-      }
+    for (int i = 0; i < 8; ++i) use(score_of(k, e.at(i)), pair(k, v0 + i));
+  };
+  auto each_logit = [&](auto use) {   // of the wave's chunks, two of them read at a time
+    for (int c = wid; c < n_ch; c += 2 * kPickWaves) {
+      Eight<DT> e0, e1;
+      const bool two = c + kPickWaves < n_ch;
+      fetch(e0, c);
+      if (two) fetch(e1, c + kPickWaves);
+      each(e0, c, use);
+      if (two) each(e1, c + kPickWaves, use);
     }
-  }
+  };
+  auto put = [&](double s, uint64_t i) {
+    const int at = atomicAdd(&n_pair, 1);
+    if (at < kPickList) list[at] = Ranked{s, i};
+  };
+  if (offers_end(tid)) put(cum[tid], pair(tid, p.end_token));
+  each_logit([&](double s, uint64_t i) {
+    if (uint32_t(order_key(s) >> 32) >= floor) put(s, i);
+  });
   __syncthreads();
   const int np = n_pair;
-  auto write = [&](int j, double s, int64_t at) {
-    const int k = int(at / a.V);
-    const int64_t v = at % a.V, o = b * p.n + j;
+  auto write = [&](int j, double s, uint64_t at) {
+    const int k = int(at >> 32);
+    const int64_t v = int64_t(at & 0xffffffffu), o = b * p.n + j;
     p.out_scores[o] = float(s);
     p.parents[o] = k;
     p.tokens[o] = v;
@@ -267,34 +347,34 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   };
   int filled = np < p.n ? np : p.n;
   if (__builtin_expect(np <= kPickList, 1)) {
-    // rank each among all (distinct positions: distinct ranks)
-    for (int t = tid; t < np; t += kPickBlock) {
-      const double s = lscore[t];
-      const int64_t at = lat[t];
-      int rank = 0;
-      for (int o = 0; o < np; ++o) rank += before(lscore[o], lat[o], s, at);
-      if (rank < p.n) write(rank, s, at);
+    // rank each among all (distinct positions: distinct ranks), 16 lanes to one
+    for (int c = tid >> 4; c < np; c += kPickGroups) {
+      const Ranked r = list[c];
+      uint32_t rank = 0;
+      for (int o = tid & 15; o < np; o += 16) {
+        const Ranked x = list[o];
+        rank += before(x.score, x.at, r.score, r.at);
+      }
+      rank += dpp_u<0xB1>(rank);
+      rank += dpp_u<0x4E>(rank);
+      rank += dpp_u<0x141>(rank);
+      rank += dpp_u<0x140>(rank);
+      if ((tid & 15) == 0 && rank < uint32_t(p.n)) write(int(rank), r.score, r.at);
     }
   } else {
     double as = INFINITY;
-    int64_t ai = -1;
+    uint64_t ai = 0;
     for (int j = 0; j < p.n; ++j) {
       double s = -INFINITY;
-      int64_t at = INT64_MAX;
-      auto offer = [&](double si, int64_t i) {
+      uint64_t at = UINT64_MAX;
+      auto offer = [&](double si, uint64_t i) {
         if (si > -INFINITY && before(as, ai, si, i) && before(si, i, s, at)) {
           s = si;
           at = i;
         }
       };
-      if (tid < p.K && ended[tid] && fabs(cum[tid]) < INFINITY) offer(cum[tid], tid * a.V + p.end_token);
-      for (int c = wid; c < n_ch; c += kPickWaves) {
-        const int item = chunks[c], k = item / n_chunk;
-        Eight<DT> e;
-        e.load(a.logits + (r0 + k) * a.row_bytes, token_at(item, 0), a.V, neg_inf<DT>());
-#pragma unroll
-        for (int i = 0; i < 8; ++i) offer(score_of(k, e.at(i)), k * a.V + token_at(item, i));
-      }
+      if (offers_end(tid)) offer(cum[tid], pair(tid, p.end_token));
+      each_logit(offer);
       workgroup_best(s, at);
       if (!(s > -INFINITY)) {
         filled = j;
@@ -320,7 +400,7 @@ void launch_select(const PickArgs& p, int64_t B, hipStream_t s) {
   const dim3 grid{unsigned((p.in.n_span + kScanBlock / 64 - 1) / (kScanBlock / 64)), unsigned(B * p.K)};
   hipLaunchKernelGGL(k_beam_scan<DT>, grid, dim3(kScanBlock), 0, s, p.in);
   if (hipPeekAtLastError() == hipSuccess)
-    hipLaunchKernelGGL(k_beam_pick<DT>, dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
+    hipLaunchKernelGGL((k_beam_pick<DT>), dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
 }
 
 // ------------------------------------------------------------- reordering
