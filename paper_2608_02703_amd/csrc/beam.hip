@@ -1,5 +1,7 @@
 // Beam search: the n best (beam, token) pairs of each sequence from rows of
 // logits, and the reordering of the states they continue.
+#include <float.h>
+
 #include "beam.h"
 #include "dev_rows.cuh"
 
@@ -186,10 +188,11 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
       top = wave_max(top);
       double s = 0.0;
       auto add = [&](const archead::BeamSpanSum& v) {
-        if (v.sum != 0.0) s += v.sum * exp(double(v.top) - double(top));
+        s += v.sum * exp(v.sum != 0.0 ? double(v.top) - double(top) : 0.0);
       };
 #pragma unroll
-      for (int u = 0; u < kPickSpans; ++u) add(first[u]);
+      for (int u = 0; u < kPickSpans; ++u)
+        if (64 * u < n_span) add(first[u]);
       for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) add(sp[i]);
       s = wave_sum(s);
       // +inf among the logits: a term inf - inf, so the sum is NaN
@@ -231,7 +234,18 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     const uint32_t key = skey[lane];
     int reach = kPickGroups;
     const int enough = p.n + p.n / 4;
-    for (int bit = 31; bit >= 0 && reach > enough; --bit) {
+    // the bits in which no two keys differ come first
+    const uint32_t some = uint32_t(__builtin_amdgcn_readfirstlane(int(key)));
+    uint32_t differ = key ^ some;
+    differ |= dpp_u<0xB1>(differ);
+    differ |= dpp_u<0x4E>(differ);
+    differ |= dpp_u<0x141>(differ);
+    differ |= dpp_u<0x140>(differ);
+    auto row = [&](int l) { return uint32_t(__builtin_amdgcn_readlane(int(differ), l)); };
+    const uint32_t all = row(0) | row(16) | row(32) | row(48);
+    const int high = all ? 31 - __builtin_clz(all) : -1;
+    floor = high == 31 ? 0u : some >> (high + 1) << (high + 1);
+    for (int bit = high; bit >= 0 && reach > enough; --bit) {
       const uint32_t t = floor | (1u << bit);
       const int c = __popcll(__ballot(key >= t));
       if (c >= p.n) {
@@ -248,7 +262,8 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     if (at < kPickList) chunks[at] = i;
   };
 #pragma unroll
-  for (int u = 0; u < kPickHeld; ++u) list_chunk(item_at(u), mine[u]);
+  for (int u = 0; u < kPickHeld; ++u)
+    if (u * kPickBlock < n_items) list_chunk(item_at(u), mine[u]);
   for (int u = kPickHeld; u * kPickBlock < n_items; ++u)
     if (item_at(u) < n_items) list_chunk(item_at(u), score_again(item_at(u)));
   __syncthreads();
@@ -331,9 +346,12 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     const int at = atomicAdd(&n_pair, 1);
     if (at < kPickList) list[at] = Ranked{s, i};
   };
+  // the least score of the floor's key (of key 1 nothing but -inf is below)
+  const uint64_t fk = uint64_t(floor) << 32;
+  const double least = floor > 1 ? __longlong_as_double((long long)(fk >> 63 ? fk ^ (uint64_t(1) << 63) : ~fk)) : -DBL_MAX;
   if (offers_end(tid)) put(cum[tid], pair(tid, p.end_token));
   each_logit([&](double s, uint64_t i) {
-    if (uint32_t(order_key(s) >> 32) >= floor) put(s, i);
+    if (s >= least) put(s, i);
   });
   __syncthreads();
   const int np = n_pair;
