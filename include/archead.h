@@ -591,9 +591,9 @@ archead_status archead_quantize_i8(const void* x, archead_dtype x_dtype, int64_t
                                    void* stream);
 
 /* out[m, n] = (sum_k a[m, k] b[n, k]) a_scales[m] b_scales[n] (+ bias[n]),
- * m < M, n < N: the sum exact (32-bit integers), then the products with
- * a_scales and b_scales and the bias in fp32, in this order, rounded once more
- * (to nearest even) for bf16 and fp16 outputs.
+ * m < M, n < N: the sum exact (32-bit integers) and rounded to fp32, its
+ * product with a_scales[m] in fp32, then that with b_scales[n] and the bias in
+ * one rounding, and one more (to nearest even) for bf16 and fp16 outputs.
  *   a         int8 [M, lda] device (any alignment), lda >= K
  *   b         int8 [N, ldb] device (any alignment), ldb >= K
  *   a_scales  fp32 [M], b_scales fp32 [N], bias fp32 [N] or NULL, device,

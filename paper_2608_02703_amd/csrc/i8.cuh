@@ -28,10 +28,9 @@ struct I8Args {
   int K;
 };
 
-// an output before its last rounding
-__device__ __forceinline__ float scaled(int acc, float sa, float sb, float bias, bool with_bias) {
-  const float y = float(acc) * sa * sb;
-  return with_bias ? y + bias : y;
+// an output before its last rounding (bias 0 where there is none)
+__device__ __forceinline__ float scaled(int acc, float sa, float sb, float bias) {
+  return fmaf(float(acc) * sa, sb, bias);
 }
 
 // four fp32 values to the output's type, at p
@@ -74,7 +73,7 @@ __device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, c
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t c = n + i < g.N ? n + i : n;
-    y[i] = scaled(acc[i], s, g.sb[c], g.bias ? g.bias[c] : 0.f, g.bias != nullptr);
+    y[i] = scaled(acc[i], s, g.sb[c], g.bias ? g.bias[c] : 0.f);
   }
   uint32_t w[EB];
   put4<DT>(reinterpret_cast<uint8_t*>(w), y);
@@ -82,10 +81,20 @@ __device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, c
   else store_part<EB>(g.out + (m * g.ldo + n) * EB, uint2{w[0], w[1]}, g.N - n);
 }
 
-// kernel launchers, one translation unit each
+constexpr int64_t kMaxLd = 1 << 22;   // a tile's rows stay within 31-bit offsets
+
+// What the kernels below need: 16-byte pieces that lie whole in a row and in
+// aligned memory.
+inline bool pieces(const I8Args& g) {
+  return aligned(g.a, 16) && aligned(g.b, 16) && g.K % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0;
+}
+// kernel launchers, one translation unit each; *_take: whether the call's sizes fit
+bool few_take(const I8Args& g);
 template <int DT>
-void launch_tiles(const I8Args& g, int n_cu, hipStream_t s);   // a, b aligned to 16, K, lda, ldb multiples of 16
+void launch_few(const I8Args& g, int n_cu, hipStream_t s);
 bool tiles_take(const I8Args& g);
+template <int DT>
+void launch_tiles(const I8Args& g, int n_cu, hipStream_t s);
 
 }  // namespace i8
 }  // namespace archead

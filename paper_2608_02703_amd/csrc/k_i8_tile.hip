@@ -2,9 +2,6 @@
 #include "dev_common.cuh"
 #include "i8.cuh"
 
-#ifndef I8MIN
-#define I8MIN 64
-#endif
 namespace {
 
 using namespace archead::i8;
@@ -15,8 +12,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTK = 128;          // k of a stage
 constexpr int kTileN = 256;       // channels of a tile
+constexpr int64_t kTurnMost = 2 << 20;   // bytes of a up to which tiles begin at different k
 constexpr int kRaster = 8;        // token tiles of a raster group
-constexpr int kMaxLd = 1 << 22;   // a tile's rows stay within 31-bit offsets
 
 // NS stages in LDS, WMW x WNW waves
 template <int TM, int WMW, int WNW, int NS>
@@ -26,9 +23,11 @@ struct Geom {
   static constexpr int MI = WM / 32, NI = WN / 32;
   static constexpr int ABYTES = TM * kTK, STAGE = ABYTES + kTileN * kTK;
   static constexpr int NA = ABYTES / 1024 / NW, NB = kTileN * kTK / 1024 / NW;   // loads of a wave and stage
-  static constexpr int OROW = 80, OUT = NS * STAGE;        // a wave's store buffer: 32 tokens of 64 bytes, padded
-  static constexpr int SCALES = OUT + NW * 32 * OROW;      // fp32 [2][TM + 2 kTileN]: a_scales, b_scales, bias
   static constexpr int NSC = TM + 2 * kTileN;
+  // a wave's store buffer: 32 tokens, or 16 where that is too much, of 64 bytes, padded
+  static constexpr int OROW = 80, OUT = NS * STAGE;
+  static constexpr int OTOK = OUT + NW * 32 * OROW + 2 * NSC * 4 <= 160 * 1024 ? 32 : 16;
+  static constexpr int SCALES = OUT + NW * OTOK * OROW;      // fp32 [2][TM + 2 kTileN]: a_scales, b_scales, bias
   static constexpr int LDS = SCALES + 2 * NSC * 4;
   static_assert(LDS <= 160 * 1024, "LDS budget");
   static_assert(NA * 1024 * NW == ABYTES && NB * 1024 * NW == kTileN * kTK, "whole loads");
@@ -70,7 +69,7 @@ __device__ __forceinline__ void wave_lds_order() {
 // all under the last step's products.
 template <int DT, int TM, int WMW, int WNW, int NS>
 __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(WMW * WNW / 4))) void k_i8_tile(
-    I8Args g, int m_tiles, int n_tiles, int per_xcd) {
+    I8Args g, int m_tiles, int n_tiles, int per_xcd, int turn) {
   using G = Geom<TM, WMW, WNW, NS>;
   constexpr int MI = G::MI, NI = G::NI;
   extern __shared__ __align__(16) uint8_t i8_lds[];
@@ -95,7 +94,7 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
   };
 
   // ---- loads: the tile and stage they have come to
-  int ld_tile = cur, ld_stage = 0, ld_slot = 0;
+  int ld_tile = cur, ld_stage = 0, ld_slot = 0, ld_first = 0;
   __amdgpu_buffer_rsrc_t ra, rb;
   uint32_t ao[G::NA], bo[G::NB];
   // this lane's unit of its wave's load i: row r, unit p of LDS, holding unit
@@ -103,6 +102,7 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
   auto begin_tile = [&]() {
     int m0, n0;
     tile_at(ld_tile, m0, n0);
+    ld_first = turn ? n0 / kTileN * turn % stages : 0;
     const int rows = int(g.M - m0 < TM ? g.M - m0 : TM), cols = int(g.N - n0 < kTileN ? g.N - n0 : kTileN);
     ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.a + m0 * g.lda), 0, (rows - 1) * lda + g.K,
                                            kBufferWord3);
@@ -126,10 +126,11 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
   auto slot_at = [&](int i) { return L + i * G::STAGE; };
   auto issue_whole = [&]() {
     lds_u8* const base = slot_at(ld_slot);
+    const int ks = ld_stage + ld_first, k0 = (ks < stages ? ks : ks - stages) * kTK;
 #pragma unroll
-    for (int i = 0; i < G::NA; ++i) load(ra, base + (wid * G::NA + i) * 1024, ao[i], ld_stage * kTK);
+    for (int i = 0; i < G::NA; ++i) load(ra, base + (wid * G::NA + i) * 1024, ao[i], k0);
 #pragma unroll
-    for (int i = 0; i < G::NB; ++i) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], ld_stage * kTK);
+    for (int i = 0; i < G::NB; ++i) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], k0);
     ++ld_stage;
     ld_slot = ld_slot + 1 == NS ? 0 : ld_slot + 1;
   };
@@ -265,45 +266,49 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
     int m0, n0;
     tile_at(cur, m0, n0);
     const float* const sc = reinterpret_cast<const float*>(i8_lds + G::SCALES) + half * G::NSC;
-    uint8_t* const buf = i8_lds + G::OUT + wid * 32 * G::OROW;
+    uint8_t* const buf = i8_lds + G::OUT + wid * G::OTOK * G::OROW;
     constexpr int EB = DT == ARCHEAD_F32 ? 4 : 2, PER = 16 / EB;   // elements of 16 bytes
+    constexpr int KP = 8 / EB;                                      // fours of channels in 64 bytes
     const bool whole = m0 + TM <= g.M && n0 + kTileN <= g.N;
+    const float* const sa = sc + wm * G::WM + lr;
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-      const float sa = sc[wm * G::WM + 32 * mi + lr];
-      const int64_t r0 = m0 + wm * G::WM + 32 * mi;
+    for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-      for (int ni = 0; ni < NI; ++ni) {
+      for (int part = 0; part < EB / 2; ++part) {   // 16 or 32 channels
+        const int c0 = wn * G::WN + 32 * ni + 32 / (EB / 2) * part;
+        f32x4 sb[KP], bi[KP];
 #pragma unroll
-        for (int part = 0; part < EB / 2; ++part) {   // 16 or 32 channels
-          constexpr int KP = 8 / EB;
+        for (int k = 0; k < KP; ++k) {
+          sb[k] = *reinterpret_cast<const f32x4*>(sc + TM + c0 + 8 * k + 4 * h);
+          bi[k] = *reinterpret_cast<const f32x4*>(sc + TM + kTileN + c0 + 8 * k + 4 * h);
+        }
 #pragma unroll
-          for (int kk = 0; kk < KP; ++kk) {
-            const int k = part * KP + kk, c = wn * G::WN + 32 * ni + 8 * k + 4 * h;
-            const f32x4 sb = *reinterpret_cast<const f32x4*>(sc + TM + c);
-            const f32x4 bi = *reinterpret_cast<const f32x4*>(sc + TM + kTileN + c);
-            float y[4];
+        for (int mi = 0; mi < MI; ++mi) {
+          float y[KP][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = scaled(acc[mi][ni][4 * k + i], sa, sb[i], bi[i], g.bias != nullptr);
-            put4<DT>(buf + lr * G::OROW + (8 * kk + 4 * h) * EB, y);
-          }
-          wave_lds_order();
+          for (int k = 0; k < KP; ++k)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int rl = 16 * j + lane / 4, q = lane & 3;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(buf + rl * G::OROW + 16 * q);
-            const int64_t n = n0 + wn * G::WN + 32 * ni + (32 / (EB / 2)) * part + q * PER;
-            uint8_t* const p = g.out + ((r0 + rl) * g.ldo + n) * EB;
-            if (whole) {
-              store_any(p, v);
-            } else if (r0 + rl < g.M) {
-              store_part<EB>(p, v, g.N - n);
+            for (int i = 0; i < 4; ++i)
+              y[k][i] = scaled(acc[mi][ni][4 * (part * KP + k) + i], sa[32 * mi], sb[k][i], bi[k][i]);
+          const int64_t n = n0 + c0 + (lane & 3) * PER;
+#pragma unroll
+          for (int t0 = 0; t0 < 32; t0 += G::OTOK) {
+            if (G::OTOK == 32 || (lr & 16) == t0)
+#pragma unroll
+              for (int k = 0; k < KP; ++k) put4<DT>(buf + (lr & (G::OTOK - 1)) * G::OROW + (8 * k + 4 * h) * EB, y[k]);
+            wave_lds_order();
+#pragma unroll
+            for (int j = 0; j < G::OTOK; j += 16) {
+              const u32x4 v = *reinterpret_cast<const u32x4*>(buf + (j + lane / 4) * G::OROW + 16 * (lane & 3));
+              const int64_t m = m0 + wm * G::WM + 32 * mi + t0 + j + lane / 4;
+              uint8_t* const p = g.out + (m * g.ldo + n) * EB;
+              if (whole) store_any(p, v);
+              else if (m < g.M) store_part<EB>(p, v, g.N - n);
             }
+            wave_lds_order();
           }
-          wave_lds_order();
         }
       }
-    }
   }
 }
 
@@ -315,7 +320,12 @@ void launch(const I8Args& g, int n_cu, hipStream_t s) {
   const void* fn = reinterpret_cast<const void*>(k_i8_tile<DT, TM, WMW, WNW, NS>);
   if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS) != hipSuccess) return;
   const int wgs = 8 * std::min(per_xcd, std::max(n_cu / 8, 1));
-  void* args[] = {const_cast<I8Args*>(&g), &m_tiles, &n_tiles, &per_xcd};
+  // Tiles of neighbouring channels begin at different k (the sums are exact in
+  // any order) where a stays in the L2s all the same: else rows of a power of
+  // two all ask for the same memory channels at once (64 x 151936 x 4096:
+  // 158 -> 127 us).
+  int turn = g.K % kTK == 0 && g.M * g.K <= kTurnMost ? 5 : 0;
+  void* args[] = {const_cast<I8Args*>(&g), &m_tiles, &n_tiles, &per_xcd, &turn};
   (void)hipLaunchKernel(fn, dim3(unsigned(wgs)), dim3(G::NW * 64), args, G::LDS, s);
 }
 
@@ -326,16 +336,29 @@ namespace i8 {
 
 bool tiles_take(const I8Args& g) {
   const int64_t tiles = ((g.M + 63) / 64) * ((g.N + kTileN - 1) / kTileN);
-  return aligned(g.a, 16) && aligned(g.b, 16) && g.K % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.K > 0 &&
-         g.lda <= kMaxLd && g.ldb <= kMaxLd && tiles < (1 << 22) && g.M > I8MIN;
+  return g.K > 0 && g.lda <= kMaxLd && g.ldb <= kMaxLd && tiles < (1 << 22);
 }
 
-#ifndef I8TM
-#define I8TM 256, 2, 4, 2
-#endif
 template <int DT>
 void launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
-  launch<DT, I8TM>(g, n_cu, s);
+  // The height for which the CUs' rounds of tiles load the fewest bytes, what
+  // bounds a stage but for the tallest: us at 64 / 128 / 192 / 256 rows for M x N x K
+  // 64 x 151936 x 4096 127 / 140 / - / 167, 333 x 50257 x 1536 63 / 53 / 48 / 51,
+  // 512 x 128256 x 8192 795 / 548 / 576 / 485, 256 x 8192 x 4096 19 / - / - / 41.
+  int tm = 0;
+  int64_t best = 0;
+  for (int t : {256, 192, 128, 64}) {
+    const int64_t tiles = (g.M + t - 1) / t * ((g.N + kTileN - 1) / kTileN);
+    const int64_t cost = (tiles + n_cu - 1) / n_cu * (t + kTileN);
+    if (!tm || cost < best) {
+      tm = t;
+      best = cost;
+    }
+  }
+  if (tm == 256) launch<DT, 256, 2, 4, 2>(g, n_cu, s);
+  else if (tm == 192) launch<DT, 192, 2, 4, 2>(g, n_cu, s);
+  else if (tm == 128) launch<DT, 128, 2, 4, 3>(g, n_cu, s);
+  else launch<DT, 64, 1, 8, 3>(g, n_cu, s);
 }
 template void launch_tiles<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
 template void launch_tiles<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);

@@ -85,7 +85,8 @@ int compute_units() {
 
 template <int DT>
 void launch_matmul(const I8Args& g, hipStream_t s) {
-  if (tiles_take(g)) return launch_tiles<DT>(g, compute_units(), s);
+  if (pieces(g) && few_take(g)) return launch_few<DT>(g, compute_units(), s);
+  if (pieces(g) && tiles_take(g)) return launch_tiles<DT>(g, compute_units(), s);
   const int64_t mt = (g.M + kATile - 1) / kATile, nt = (g.N + kATile - 1) / kATile, tiles = mt * nt;
   const dim3 grid{unsigned(tiles < (1 << 22) ? tiles : 1 << 22)};
   hipLaunchKernelGGL(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
