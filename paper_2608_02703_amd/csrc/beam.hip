@@ -84,14 +84,16 @@ __device__ __forceinline__ double wave_sum(double v) {
   return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
 }
 
-// a wave to a span: its chunks' largest logits, its sum of exponentials
+// whether a row's logits say anything
+__device__ __forceinline__ bool row_counts(const ScanArgs& a, int64_t r) {
+  return fabsf(a.scores[r]) < INFINITY && !(a.finished && a.finished[r]);
+}
+
+// Span sp of row r, by a wave: its chunks' largest logits to cmax[0 ..
+// kSpanChunks), its sum of exponentials to *span.
 template <int DT>
-__global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int wid = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  const int64_t r = blockIdx.y, sp = int64_t(blockIdx.x) * (kScanBlock / 64) + wid;
-  if (sp >= a.n_span) return;
-  if (!(fabsf(a.scores[r]) < INFINITY) || (a.finished && a.finished[r])) return;   // its logits say nothing
+__device__ __forceinline__ void scan_span(const ScanArgs& a, int64_t r, int64_t sp, int lane, float* cmax,
+                                          archead::BeamSpanSum* span) {
   const uint8_t* row = a.logits + r * a.row_bytes;
   Eight<DT> e[kSpanChunks];
 #pragma unroll
@@ -114,14 +116,25 @@ __global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f((e[c].at(i) - ref) * 1.4426950408889634f);
   const double sd = wave_sum(double(s));
-  if (lane == 0) a.span[r * a.n_span + sp] = archead::BeamSpanSum{sd, ref};
+  if (lane == 0) *span = archead::BeamSpanSum{sd, ref};
   if (lane < kSpanChunks) {
     float m = cm[0];
 #pragma unroll
     for (int c = 1; c < kSpanChunks; ++c) m = lane == c ? cm[c] : m;
-    a.cmax[(r * a.n_span + sp) * kSpanChunks + lane] = m;
+    cmax[lane] = m;
   }
 }
+
+template <int DT>
+__global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int64_t r = blockIdx.y, sp = int64_t(blockIdx.x) * (kScanBlock / 64) + wid;
+  if (sp >= a.n_span || !row_counts(a, r)) return;
+  const int64_t i = r * a.n_span + sp;
+  scan_span<DT>(a, r, sp, lane, a.cmax + i * kSpanChunks, a.span + i);
+}
+
 constexpr int kPickBlock = 1024, kPickWaves = kPickBlock / 64;
 constexpr int kPickHeld = 4;     // chunks whose largest logits a thread keeps
 constexpr int kPickSpans = 4;    // spans whose sums a lane keeps
@@ -148,8 +161,12 @@ __device__ __forceinline__ bool before(double sa, uint64_t ia, double sb, uint64
   return sa > sb || (sa == sb && ia < ib);
 }
 
-template <int DT>
+// FEW: no more spans in a sequence than waves, which read them here (no first
+// launch)
+template <int DT, bool FEW>
 __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
+  __shared__ float few_cmax[FEW ? kPickWaves * kSpanChunks : 1];
+  __shared__ archead::BeamSpanSum few_span[FEW ? kPickWaves : 1];
   __shared__ double lse[ARCHEAD_BEAM_MAX], cum[ARCHEAD_BEAM_MAX];   // lse: NaN where a row offers nothing by its logits
   __shared__ bool ended[ARCHEAD_BEAM_MAX];
   __shared__ uint32_t skey[kPickGroups];
@@ -164,18 +181,31 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   const int64_t b = blockIdx.x, r0 = b * p.K;
   const int n_span = int(a.n_span), n_chunk = n_span * kSpanChunks, n_items = n_chunk * p.K;   // (K V / 512 < 2^27)
   if (tid == 0) n_list = n_pair = 0;
+  if constexpr (FEW) {
+    const int k = wid / n_span;
+    if (k < p.K && row_counts(a, r0 + k))
+      scan_span<DT>(a, r0 + k, wid - k * n_span, lane, few_cmax + wid * kSpanChunks, few_span + wid);
+    __syncthreads();
+  }
+  auto cmax_of = [&](int item) {
+    if constexpr (FEW) return few_cmax[item];
+    else return a.cmax[r0 * n_chunk + item];
+  };
+  auto span_of = [&](int k, int i) {
+    if constexpr (FEW) return few_span[k * n_span + i];
+    else return a.span[(r0 + k) * a.n_span + i];
+  };
   // item i of u: chunk i % n_chunk of beam i / n_chunk; neighbouring items go
   // to different groups of 16 threads
   auto item_at = [&](int u) { return u * kPickBlock + (tid & 15) * kPickGroups + (tid >> 4); };
   float held[kPickHeld];   // (of rows that say nothing: whatever the workspace holds)
 #pragma unroll
-  for (int u = 0; u < kPickHeld; ++u) held[u] = item_at(u) < n_items ? a.cmax[r0 * n_chunk + item_at(u)] : -INFINITY;
+  for (int u = 0; u < kPickHeld; ++u) held[u] = item_at(u) < n_items ? cmax_of(item_at(u)) : -INFINITY;
   for (int k = wid; k < p.K; k += kPickWaves) {
-    const archead::BeamSpanSum* const sp = a.span + (r0 + k) * a.n_span;
     archead::BeamSpanSum first[kPickSpans];
 #pragma unroll
     for (int u = 0; u < kPickSpans; ++u)
-      first[u] = lane + 64 * u < n_span ? sp[lane + 64 * u] : archead::BeamSpanSum{0.0, 0.f};
+      first[u] = lane + 64 * u < n_span ? span_of(k, lane + 64 * u) : archead::BeamSpanSum{0.0, 0.f};
     const float c = a.scores[r0 + k];
     const bool f = a.finished && a.finished[r0 + k];
     double l = NAN;
@@ -184,7 +214,10 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
       float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kPickSpans; ++u) top = first[u].sum != 0.0 ? fmaxf(top, first[u].top) : top;
-      for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) top = sp[i].sum != 0.0 ? fmaxf(top, sp[i].top) : top;
+      for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) {
+        const archead::BeamSpanSum v = span_of(k, i);
+        top = v.sum != 0.0 ? fmaxf(top, v.top) : top;
+      }
       top = wave_max(top);
       double s = 0.0;
       auto add = [&](const archead::BeamSpanSum& v) {
@@ -193,7 +226,7 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
 #pragma unroll
       for (int u = 0; u < kPickSpans; ++u)
         if (64 * u < n_span) add(first[u]);
-      for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) add(sp[i]);
+      for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) add(span_of(k, i));
       s = wave_sum(s);
       // +inf among the logits: a term inf - inf, so the sum is NaN
       if (s > 0.0) l = top + log(s);
@@ -210,7 +243,7 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     const int k = item / n_chunk;
     return lse[k] == lse[k] ? score_of(k, top) : double(-INFINITY);
   };
-  auto score_again = [&](int item) { return chunk_score(item, a.cmax[r0 * n_chunk + item]); };
+  auto score_again = [&](int item) { return chunk_score(item, cmax_of(item)); };
   // ---- a floor: about the n-th largest of the groups' best chunks, in the
   // order's first 32 bits
   double mine[kPickHeld];
@@ -415,10 +448,14 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
 
 template <int DT>
 void launch_select(const PickArgs& p, int64_t B, hipStream_t s) {
+  if (p.in.n_span * p.K <= kPickWaves) {
+    hipLaunchKernelGGL((k_beam_pick<DT, true>), dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
+    return;
+  }
   const dim3 grid{unsigned((p.in.n_span + kScanBlock / 64 - 1) / (kScanBlock / 64)), unsigned(B * p.K)};
   hipLaunchKernelGGL(k_beam_scan<DT>, grid, dim3(kScanBlock), 0, s, p.in);
   if (hipPeekAtLastError() == hipSuccess)
-    hipLaunchKernelGGL((k_beam_pick<DT>), dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
+    hipLaunchKernelGGL((k_beam_pick<DT, false>), dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
 }
 
 // ------------------------------------------------------------- reordering

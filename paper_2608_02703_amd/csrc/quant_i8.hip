@@ -5,57 +5,71 @@ namespace {
 
 using namespace archead::rows;
 
-constexpr int kQBlock = 256;
-constexpr int kQHeld = 8;   // groups of 8 elements a thread keeps between its two passes
+constexpr int kQMost = 1024;     // threads of a workgroup
+constexpr int kQShort = 512;     // longest row that 16 lanes take
 
-// TPR threads to a row (64: a wave each, 256: the workgroup).  One pass over
-// the row for the largest magnitude, compared as integers (so a NaN or an
-// infinity is the largest), and one for the codes; up to 64 TPR elements stay
-// in registers in between, longer rows are read again (from the caches).
+// SHORT: 16 lanes to a row, four rows to a wave; else a workgroup to a row, as
+// many threads as hold it in HELD groups of 8 elements each.  One pass over the row for the
+// largest magnitude, compared as integers (so a NaN or an infinity is the
+// largest), and one for the codes; what a thread holds stays in registers in
+// between, longer rows are read again (from the caches).  151936 x 4096 bf16:
+// 312 us (6.0 TB/s); a wave to a row, eight groups a lane: 443.
 //
-// With s the scale, q = rint(x * (1 / s)) is the nearest integer to x / s or
-// next to it.  r = x - q s is exact (a multiple of the smaller of the two
-// operands' units, and at most about s / 2), so comparing it with s / 2 (exact)
-// says which integer is nearest, and which way a half goes.
-template <int DT, int TPR>
-__global__ __launch_bounds__(kQBlock) void k_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes,
+// With s the scale, x * (1 / s) + 1.5 * 2^23 (one rounding) ends in the integer
+// q nearest to x / s or next to it, in two's complement.  r = x - q s is exact (a
+// multiple of the smaller of the two operands' units, and at most about s / 2),
+// so comparing it with s / 2 (exact) says which integer is nearest, and which way
+// a half goes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {   // another lane of the row of 16
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false));
+}
+
+template <int DT, bool SHORT, int HELD>
+__global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes,
                                                       int8_t* codes, int64_t ldc, float* scales) {
   using E = Eight<DT>;
-  constexpr int kRows = kQBlock / TPR;
-  __shared__ uint32_t smax[2][kQBlock / 64];
-  const int tid = threadIdx.x, t = tid % TPR;
+  static_assert(!SHORT || HELD * 128 == kQShort, "a short row is held whole");
+  const int TPR = SHORT ? 16 : int(blockDim.x), rows = SHORT ? int(blockDim.x) / 16 : 1;
+  __shared__ uint32_t smax[2][kQMost / 64];
+  const int tid = threadIdx.x, t = SHORT ? tid & 15 : tid;
   int turn = 0;
-  for (int64_t m0 = int64_t(blockIdx.x) * kRows; m0 < M; m0 += int64_t(gridDim.x) * kRows, turn ^= 1) {
-    const int64_t m = m0 + tid / TPR;
-    const bool live = m < M;   // (a wave's rows are its own: uniform)
+  for (int64_t m0 = int64_t(blockIdx.x) * rows; m0 < M; m0 += int64_t(gridDim.x) * rows, turn ^= 1) {
+    const int64_t m = SHORT ? m0 + (tid >> 4) : m0;
+    const bool live = m < M;
     const uint8_t* row = x + m * row_bytes;
     const int64_t n = live ? d : 0;
-    E held[kQHeld];
+    E held[HELD];
     uint32_t top = 0;
     auto larger = [&](const E& e) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(e.at(i)) & 0x7fffffffu);
     };
 #pragma unroll
-    for (int g = 0; g < kQHeld; ++g) {
+    for (int g = 0; g < HELD; ++g) {
       const int64_t j = (int64_t(g) * TPR + t) * 8;
       if (j < n) held[g].load(row, j, n, 0);
     }
 #pragma unroll
-    for (int g = 0; g < kQHeld; ++g)
+    for (int g = 0; g < HELD; ++g)
       if ((int64_t(g) * TPR + t) * 8 < n) larger(held[g]);
-    for (int64_t j = (int64_t(kQHeld) * TPR + t) * 8; j < n; j += TPR * 8) {
+    for (int64_t j = (int64_t(HELD) * TPR + t) * 8; j < n; j += TPR * 8) {
       E e;
       e.load(row, j, n, 0);
       larger(e);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), o, 64)));
-    if constexpr (TPR > 64) {
+    top = max(top, dpp<0xB1>(top));
+    top = max(top, dpp<0x4E>(top));
+    top = max(top, dpp<0x141>(top));
+    top = max(top, dpp<0x140>(top));
+    if constexpr (!SHORT) {
+      auto of = [&](int l) { return uint32_t(__builtin_amdgcn_readlane(int(top), l)); };
+      top = max(max(of(0), of(16)), max(of(32), of(48)));
+    }
+    if (!SHORT && TPR > 64) {
       if ((tid & 63) == 0) smax[turn][tid >> 6] = top;
       __syncthreads();   // (the other of the two is read no more)
-#pragma unroll
-      for (int w = 0; w < kQBlock / 64; ++w) top = max(top, smax[turn][w]);
+      for (int w = 0; w < TPR / 64; ++w) top = max(top, smax[turn][w]);
     }
     if (!live) continue;
     const bool finite = top < 0x7f800000u;
@@ -63,26 +77,31 @@ __global__ __launch_bounds__(kQBlock) void k_quantize(const uint8_t* x, int64_t 
     const float inv = finite ? 1.f / s : 0.f, half = 0.5f * s;
     if (t == 0) scales[m] = s;
     int8_t* out = codes + m * ldc;
+    constexpr float kBig = 0x1.8p23f;
     auto write = [&](const E& e, int64_t j) {
-      float q[8], r[8], far = 0.f;
+      float t[8], r[8], far = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float v = finite ? e.at(i) : 0.f;
-        q[i] = rintf(v * inv);
-        r[i] = fmaf(-q[i], s, v);
+        const float v = e.at(i);
+        t[i] = fmaf(v, inv, kBig);
+        r[i] = fmaf(kBig - t[i], s, v);
         far = fmaxf(far, fabsf(r[i]));
       }
       if (__builtin_expect(far >= half, 0)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const bool odd = int(q[i]) & 1;
-          if (r[i] > half || (r[i] == half && odd)) q[i] += 1.f;
-          else if (r[i] < -half || (r[i] == -half && odd)) q[i] -= 1.f;
+          const bool odd = __float_as_uint(t[i]) & 1;
+          if (r[i] > half || (r[i] == half && odd)) t[i] += 1.f;
+          else if (r[i] < -half || (r[i] == -half && odd)) t[i] -= 1.f;
         }
       }
-      uint32_t w[2] = {0, 0};
+      uint32_t w[2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t(int(q[i])) & 0xffu) << (8 * (i % 4));
+      for (int i = 0; i < 2; ++i) {   // the low bytes of four
+        auto low = [&](int k) { return __float_as_uint(t[4 * i + k]); };
+        const uint32_t a = __builtin_amdgcn_perm(low(1), low(0), 0x0c0c0400), b = __builtin_amdgcn_perm(low(3), low(2), 0x0c0c0400);
+        w[i] = finite ? a | b << 16 : 0u;
+      }
       if (j + 8 <= d) {
         store_any(out + j, uint2{w[0], w[1]});
       } else {
@@ -90,11 +109,11 @@ __global__ __launch_bounds__(kQBlock) void k_quantize(const uint8_t* x, int64_t 
       }
     };
 #pragma unroll
-    for (int g = 0; g < kQHeld; ++g) {
+    for (int g = 0; g < HELD; ++g) {
       const int64_t j = (int64_t(g) * TPR + t) * 8;
       if (j < d) write(held[g], j);
     }
-    for (int64_t j = (int64_t(kQHeld) * TPR + t) * 8; j < d; j += TPR * 8) {
+    for (int64_t j = (int64_t(HELD) * TPR + t) * 8; j < d; j += TPR * 8) {
       E e;
       e.load(row, j, d, 0);
       write(e, j);
@@ -102,14 +121,23 @@ __global__ __launch_bounds__(kQBlock) void k_quantize(const uint8_t* x, int64_t 
   }
 }
 
+template <int DT, bool SHORT, int HELD>
+void launch_rows(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc, float* scales,
+                 hipStream_t s) {
+  const int64_t groups = SHORT ? (M + 15) / 16 : M, waves = SHORT ? 4 : (d + 512 * HELD - 1) / (512 * HELD);
+  const int64_t most = kQMost / 64;
+  hipLaunchKernelGGL((k_quantize<DT, SHORT, HELD>), dim3(unsigned(groups < (1 << 22) ? groups : 1 << 22)),
+                     dim3(unsigned(64 * (waves < most ? waves : most))), 0, s, x, M, d, row_bytes, codes, ldc, scales);
+}
 template <int DT>
 void launch_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc,
                      float* scales, hipStream_t s) {
-  const bool waves = d <= 64 * 8 * kQHeld && M >= 1024;
-  const int64_t need = waves ? (M + 3) / 4 : M;
-  const dim3 grid{unsigned(need < (1 << 22) ? need : 1 << 22)};
-  if (waves) hipLaunchKernelGGL((k_quantize<DT, 64>), grid, dim3(kQBlock), 0, s, x, M, d, row_bytes, codes, ldc, scales);
-  else hipLaunchKernelGGL((k_quantize<DT, 256>), grid, dim3(kQBlock), 0, s, x, M, d, row_bytes, codes, ldc, scales);
+  // Fewer waves with more in flight each where there are plenty: us with 2 / 4
+  // groups 151936 x 4096 336 / 312, 16384 x 8192 88 / 74, 4096 x 4096 12.7 / 13.3,
+  // 300 x 4096 4.5 / 5.8.
+  if (d <= kQShort) launch_rows<DT, true, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
+  else if (M * d < (1 << 26)) launch_rows<DT, false, 2>(x, M, d, row_bytes, codes, ldc, scales, s);
+  else launch_rows<DT, false, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
 }
 
 }  // namespace
