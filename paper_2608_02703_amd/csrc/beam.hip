@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   __shared__ archead::BeamSpanSum few_span[FEW ? kPickWaves : 1];
   __shared__ double lse[ARCHEAD_BEAM_MAX], cum[ARCHEAD_BEAM_MAX];   // lse: NaN where a row offers nothing by its logits
   __shared__ bool ended[ARCHEAD_BEAM_MAX];
-  __shared__ uint32_t skey[kPickGroups];
+  __shared__ uint32_t skey[kPickGroups], lane_key[kPickBlock];
   __shared__ Ranked list[kPickList];
   __shared__ int chunks[kPickList];
   __shared__ double wscore[kPickWaves];
@@ -379,15 +379,50 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     const int at = atomicAdd(&n_pair, 1);
     if (at < kPickList) list[at] = Ranked{s, i};
   };
-  // the least score of the floor's key (of key 1 nothing but -inf is below)
-  const uint64_t fk = uint64_t(floor) << 32;
-  const double least = floor > 1 ? __longlong_as_double((long long)(fk >> 63 ? fk ^ (uint64_t(1) << 63) : ~fk)) : -DBL_MAX;
+  // the least score whose order begins with f (below 1: -inf alone)
+  auto score_at = [](uint32_t f) {
+    const uint64_t k = uint64_t(f) << 32;
+    return f > 1 ? __longlong_as_double((long long)(k >> 63 ? k ^ (uint64_t(1) << 63) : ~k)) : -DBL_MAX;
+  };
+  const double least = score_at(floor);
   if (offers_end(tid)) put(cum[tid], pair(tid, p.end_token));
   each_logit([&](double s, uint64_t i) {
     if (s >= least) put(s, i);
   });
   __syncthreads();
-  const int np = n_pair;
+  int np = n_pair;
+  if (__builtin_expect(np > kPickList, 0)) {
+    // Too many (few chunks, or the best logits side by side): a second floor,
+    // about the n-th largest of the lanes' best pairs, and those that reach it.
+    uint32_t top = offers_end(tid) ? uint32_t(order_key(cum[tid]) >> 32) : 0u;
+    each_logit([&](double s, uint64_t) { top = max(top, uint32_t(order_key(s) >> 32)); });
+    lane_key[tid] = top;
+    __syncthreads();
+    if (tid == 0) n_pair = 0;
+    uint32_t kk[kPickWaves];
+#pragma unroll
+    for (int i = 0; i < kPickWaves; ++i) kk[i] = lane_key[64 * i + lane];
+    uint32_t f = 0;
+    int reach = kPickBlock;
+    for (int bit = 31; bit >= 0 && reach > p.n + p.n / 4; --bit) {
+      const uint32_t t = f | (1u << bit);
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kPickWaves; ++i) c += __popcll(__ballot(kk[i] >= t));
+      if (c >= p.n) {
+        f = t;
+        reach = c;
+      }
+    }
+    const double least2 = score_at(max(f, 1u));
+    __syncthreads();
+    if (offers_end(tid) && cum[tid] >= least2) put(cum[tid], pair(tid, p.end_token));
+    each_logit([&](double s, uint64_t i) {
+      if (s >= least2) put(s, i);
+    });
+    __syncthreads();
+    np = n_pair;
+  }
   auto write = [&](int j, double s, uint64_t at) {
     const int k = int(at >> 32);
     const int64_t v = int64_t(at & 0xffffffffu), o = b * p.n + j;
