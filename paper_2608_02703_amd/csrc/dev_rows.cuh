@@ -5,6 +5,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <tuple>
+
 #include "internal.h"
 
 namespace archead {
@@ -72,6 +74,26 @@ struct Eight {
     }
   }
 };
+
+// fn<<<grid, block, lds, s>>>(args...), its own status returned (the thread's last
+// error may be another call's)
+template <typename... P, typename... A>
+hipError_t launch_kernel(void (*fn)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t s, const A&... args) {
+  std::tuple<P...> held(args...);
+  return std::apply(
+      [&](P&... h) {
+        void* ptrs[] = {static_cast<void*>(&h)...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(fn), grid, block, ptrs, lds, s);
+      },
+      held);
+}
+// the same with more than 64 KB of LDS
+template <typename... P, typename... A>
+hipError_t launch_kernel_lds(void (*fn)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t s, const A&... args) {
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+  return e == hipSuccess ? launch_kernel(fn, grid, block, lds, s, args...) : e;
+}
 
 inline bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline int dtype_bytes(archead_dtype t) { return t == ARCHEAD_F32 ? 4 : 2; }

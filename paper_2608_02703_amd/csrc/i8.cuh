@@ -91,10 +91,10 @@ inline bool pieces(const I8Args& g) {
 // kernel launchers, one translation unit each; *_take: whether the call's sizes fit
 bool few_take(const I8Args& g);
 template <int DT>
-void launch_few(const I8Args& g, int n_cu, hipStream_t s);
+hipError_t launch_few(const I8Args& g, int n_cu, hipStream_t s);
 bool tiles_take(const I8Args& g);
 template <int DT>
-void launch_tiles(const I8Args& g, int n_cu, hipStream_t s);
+hipError_t launch_tiles(const I8Args& g, int n_cu, hipStream_t s);
 
 }  // namespace i8
 }  // namespace archead

@@ -161,26 +161,22 @@ bool few_take(const I8Args& g) {
 
 namespace {
 template <int DT, int NS>
-void launch_as(const I8Args& g, int n_cu, hipStream_t s) {
-  const void* fn = reinterpret_cast<const void*>(k_i8_few<DT, NS>);
-  const int lds = int(g.M * a_row(g.K)) + kFWaves * wave_lds(NS);
-  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return;
-  int64_t units = (g.N + kFRows - 1) / kFRows;
-  const int64_t need = (units + kFWaves - 1) / kFWaves;
-  void* args[] = {const_cast<I8Args*>(&g), &units};
-  (void)hipLaunchKernel(fn, dim3(unsigned(need < n_cu ? need : n_cu)), dim3(kFWaves * 64), args, lds, s);
+hipError_t launch_as(const I8Args& g, int n_cu, hipStream_t s) {
+  const int64_t units = (g.N + kFRows - 1) / kFRows, need = (units + kFWaves - 1) / kFWaves;
+  return launch_kernel_lds(k_i8_few<DT, NS>, dim3(unsigned(need < n_cu ? need : n_cu)), dim3(kFWaves * 64),
+                           size_t(g.M * a_row(g.K)) + kFWaves * wave_lds(NS), s, g, units);
 }
 }  // namespace
 
 template <int DT>
-void launch_few(const I8Args& g, int n_cu, hipStream_t s) {
+hipError_t launch_few(const I8Args& g, int n_cu, hipStream_t s) {
   // three stages a wave where a leaves them room
-  if (g.M * a_row(g.K) + kFWaves * wave_lds(3) <= kFLds) launch_as<DT, 3>(g, n_cu, s);
-  else launch_as<DT, 2>(g, n_cu, s);
+  if (g.M * a_row(g.K) + kFWaves * wave_lds(3) <= kFLds) return launch_as<DT, 3>(g, n_cu, s);
+  return launch_as<DT, 2>(g, n_cu, s);
 }
-template void launch_few<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
-template void launch_few<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
-template void launch_few<ARCHEAD_F16>(const I8Args&, int, hipStream_t);
+template hipError_t launch_few<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
+template hipError_t launch_few<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
+template hipError_t launch_few<ARCHEAD_F16>(const I8Args&, int, hipStream_t);
 
 }  // namespace i8
 }  // namespace archead

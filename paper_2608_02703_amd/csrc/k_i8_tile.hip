@@ -313,20 +313,17 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
 }
 
 template <int DT, int TM, int WMW, int WNW, int NS>
-void launch(const I8Args& g, int n_cu, hipStream_t s) {
+hipError_t launch(const I8Args& g, int n_cu, hipStream_t s) {
   using G = Geom<TM, WMW, WNW, NS>;
-  int m_tiles = int((g.M + TM - 1) / TM), n_tiles = int((g.N + kTileN - 1) / kTileN);
-  int per_xcd = (m_tiles * n_tiles + 7) / 8;
-  const void* fn = reinterpret_cast<const void*>(k_i8_tile<DT, TM, WMW, WNW, NS>);
-  if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS) != hipSuccess) return;
-  const int wgs = 8 * std::min(per_xcd, std::max(n_cu / 8, 1));
+  const int m_tiles = int((g.M + TM - 1) / TM), n_tiles = int((g.N + kTileN - 1) / kTileN);
+  const int per_xcd = (m_tiles * n_tiles + 7) / 8, wgs = 8 * std::min(per_xcd, std::max(n_cu / 8, 1));
   // Tiles of neighbouring channels begin at different k (the sums are exact in
   // any order) where a stays in the L2s all the same: else rows of a power of
   // two all ask for the same memory channels at once (64 x 151936 x 4096:
   // 158 -> 127 us).
-  int turn = g.K % kTK == 0 && g.M * g.K <= kTurnMost ? 5 : 0;
-  void* args[] = {const_cast<I8Args*>(&g), &m_tiles, &n_tiles, &per_xcd, &turn};
-  (void)hipLaunchKernel(fn, dim3(unsigned(wgs)), dim3(G::NW * 64), args, G::LDS, s);
+  const int turn = g.K % kTK == 0 && g.M * g.K <= kTurnMost ? 5 : 0;
+  return launch_kernel_lds(k_i8_tile<DT, TM, WMW, WNW, NS>, dim3(unsigned(wgs)), dim3(G::NW * 64), G::LDS, s, g, m_tiles,
+                           n_tiles, per_xcd, turn);
 }
 
 }  // namespace
@@ -340,7 +337,7 @@ bool tiles_take(const I8Args& g) {
 }
 
 template <int DT>
-void launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
+hipError_t launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
   // The height for which the CUs' rounds of tiles load the fewest bytes, what
   // bounds a stage but for the tallest: us at 64 / 128 / 192 / 256 rows for M x N x K
   // 64 x 151936 x 4096 127 / 140 / - / 167, 333 x 50257 x 1536 63 / 53 / 48 / 51,
@@ -355,14 +352,14 @@ void launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
       best = cost;
     }
   }
-  if (tm == 256) launch<DT, 256, 2, 4, 2>(g, n_cu, s);
-  else if (tm == 192) launch<DT, 192, 2, 4, 2>(g, n_cu, s);
-  else if (tm == 128) launch<DT, 128, 2, 4, 3>(g, n_cu, s);
-  else launch<DT, 64, 1, 8, 3>(g, n_cu, s);
+  return tm == 256   ? launch<DT, 256, 2, 4, 2>(g, n_cu, s)
+         : tm == 192 ? launch<DT, 192, 2, 4, 2>(g, n_cu, s)
+         : tm == 128 ? launch<DT, 128, 2, 4, 3>(g, n_cu, s)
+                     : launch<DT, 64, 1, 8, 3>(g, n_cu, s);
 }
-template void launch_tiles<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
-template void launch_tiles<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
-template void launch_tiles<ARCHEAD_F16>(const I8Args&, int, hipStream_t);
+template hipError_t launch_tiles<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
+template hipError_t launch_tiles<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
+template hipError_t launch_tiles<ARCHEAD_F16>(const I8Args&, int, hipStream_t);
 
 }  // namespace i8
 }  // namespace archead

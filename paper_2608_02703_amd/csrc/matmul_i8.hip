@@ -84,12 +84,19 @@ int compute_units() {
 }
 
 template <int DT>
-void launch_matmul(const I8Args& g, hipStream_t s) {
-  if (pieces(g) && few_take(g)) return launch_few<DT>(g, compute_units(), s);
-  if (pieces(g) && tiles_take(g)) return launch_tiles<DT>(g, compute_units(), s);
+hipError_t launch_matmul(const I8Args& g, hipStream_t s) {
+  if (pieces(g)) {
+    const int n_cu = compute_units();
+    // From 9 tokens on the tiles' stores of 64 bytes and more of a token tell,
+    // where there is a tile for every CU: us of the two M = 8 / 16 at N = 262144,
+    // K = 2560 121 / 127 and 120 / 122; M = 8 at N = 16384, K = 4096 14 and 23.
+    const bool few = few_take(g) && (g.M <= 8 || (g.N + 255) / 256 < n_cu || !tiles_take(g));
+    if (few) return launch_few<DT>(g, n_cu, s);
+    if (tiles_take(g)) return launch_tiles<DT>(g, n_cu, s);
+  }
   const int64_t mt = (g.M + kATile - 1) / kATile, nt = (g.N + kATile - 1) / kATile, tiles = mt * nt;
   const dim3 grid{unsigned(tiles < (1 << 22) ? tiles : 1 << 22)};
-  hipLaunchKernelGGL(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
+  return launch_kernel(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
 }
 
 }  // namespace
@@ -113,8 +120,8 @@ extern "C" archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const 
     return fail(ARCHEAD_E_MISALIGNED, "scales / bias / out misaligned");
   const I8Args g{a, b, a_scales, b_scales, bias, static_cast<uint8_t*>(out), lda, ldb, ldo, M, N, int(K)};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (out_dtype == ARCHEAD_F32) launch_matmul<ARCHEAD_F32>(g, s);
-  else if (out_dtype == ARCHEAD_BF16) launch_matmul<ARCHEAD_BF16>(g, s);
-  else launch_matmul<ARCHEAD_F16>(g, s);
-  return launch_status(hipGetLastError(), "int8 product launch");
+  const hipError_t e = out_dtype == ARCHEAD_F32    ? launch_matmul<ARCHEAD_F32>(g, s)
+                       : out_dtype == ARCHEAD_BF16 ? launch_matmul<ARCHEAD_BF16>(g, s)
+                                                   : launch_matmul<ARCHEAD_F16>(g, s);
+  return launch_status(e, "int8 product launch");
 }

@@ -122,22 +122,22 @@ __global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t
 }
 
 template <int DT, bool SHORT, int HELD>
-void launch_rows(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc, float* scales,
+hipError_t launch_rows(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc, float* scales,
                  hipStream_t s) {
   const int64_t groups = SHORT ? (M + 15) / 16 : M, waves = SHORT ? 4 : (d + 512 * HELD - 1) / (512 * HELD);
   const int64_t most = kQMost / 64;
-  hipLaunchKernelGGL((k_quantize<DT, SHORT, HELD>), dim3(unsigned(groups < (1 << 22) ? groups : 1 << 22)),
-                     dim3(unsigned(64 * (waves < most ? waves : most))), 0, s, x, M, d, row_bytes, codes, ldc, scales);
+  return launch_kernel(k_quantize<DT, SHORT, HELD>, dim3(unsigned(groups < (1 << 22) ? groups : 1 << 22)),
+                       dim3(unsigned(64 * (waves < most ? waves : most))), 0, s, x, M, d, row_bytes, codes, ldc, scales);
 }
 template <int DT>
-void launch_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc,
+hipError_t launch_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc,
                      float* scales, hipStream_t s) {
   // Fewer waves with more in flight each where there are plenty: us with 2 / 4
   // groups 151936 x 4096 336 / 312, 16384 x 8192 88 / 74, 4096 x 4096 12.7 / 13.3,
   // 300 x 4096 4.5 / 5.8.
-  if (d <= kQShort) launch_rows<DT, true, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
-  else if (M * d < (1 << 26)) launch_rows<DT, false, 2>(x, M, d, row_bytes, codes, ldc, scales, s);
-  else launch_rows<DT, false, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
+  if (d <= kQShort) return launch_rows<DT, true, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
+  if (M * d < (1 << 26)) return launch_rows<DT, false, 2>(x, M, d, row_bytes, codes, ldc, scales, s);
+  return launch_rows<DT, false, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
 }
 
 }  // namespace
@@ -158,8 +158,8 @@ extern "C" archead_status archead_quantize_i8(const void* x, archead_dtype x_dty
   const uint8_t* xb = static_cast<const uint8_t*>(x);
   const int64_t row_bytes = ldx * dtype_bytes(x_dtype);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (x_dtype == ARCHEAD_F32) launch_quantize<ARCHEAD_F32>(xb, M, d, row_bytes, codes, ldc, scales, s);
-  else if (x_dtype == ARCHEAD_BF16) launch_quantize<ARCHEAD_BF16>(xb, M, d, row_bytes, codes, ldc, scales, s);
-  else launch_quantize<ARCHEAD_F16>(xb, M, d, row_bytes, codes, ldc, scales, s);
-  return launch_status(hipGetLastError(), "quantize launch");
+  const hipError_t e = x_dtype == ARCHEAD_F32    ? launch_quantize<ARCHEAD_F32>(xb, M, d, row_bytes, codes, ldc, scales, s)
+                       : x_dtype == ARCHEAD_BF16 ? launch_quantize<ARCHEAD_BF16>(xb, M, d, row_bytes, codes, ldc, scales, s)
+                                                 : launch_quantize<ARCHEAD_F16>(xb, M, d, row_bytes, codes, ldc, scales, s);
+  return launch_status(e, "quantize launch");
 }

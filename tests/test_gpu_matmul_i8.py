@@ -192,6 +192,29 @@ def test_matmul_output_rows(M, dtype, N, ldo, off):
     assert (flat[mask] == -7.0).all()
 
 
+# More tiles than CUs, so that workgroups take several and their loads run on
+# from one to the next: every tile height, stages of one tile up to more than are
+# in flight, K that ends inside a stage.
+@pytest.mark.parametrize("K", [16, 128, 256, 272, 400, 640, 1040])
+@pytest.mark.parametrize("M,N", [(40, 70001), (120, 66000), (180, 67003), (250, 66500)])
+def test_matmul_many_tiles(M, N, K):
+    _run_product(M, N, K, "bf16", True, seed=K)
+
+
+@pytest.mark.parametrize("M,N,K", [(4100, 5003, 640), (2049, 9001, 1152), (700, 30011, 144)])
+def test_matmul_many_tiles_of_many_tokens(M, N, K):
+    _run_product(M, N, K, "f16", False, seed=M)
+
+
+# Several units of channels a wave: one stage to a unit and more, both ring
+# depths (the second where a is large)
+@pytest.mark.parametrize("M,N,K", [(1, 70001, 16), (3, 70001, 256), (8, 40003, 272), (5, 34005, 528), (16, 33001, 1040),
+                                   (7, 33001, 2064), (8, 3001, 8192), (2, 2000, 16384), (16, 5000, 4096), (4, 50257, 1536)])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_matmul_few_tokens(M, N, K, dtype):
+    _run_product(M, N, K, dtype, M % 2 == 1, seed=N)
+
+
 @pytest.mark.parametrize("M,N", [(1, 33), (20, 33), (70, 260), (300, 260)])
 def test_matmul_largest_sums(M, N):
     """K at its limit with all codes -128: 131071 * 2^14 < 2^31."""
