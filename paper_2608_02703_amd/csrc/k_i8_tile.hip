@@ -15,22 +15,22 @@ constexpr int kTileN = 256;       // channels of a tile
 constexpr int64_t kTurnMost = 2 << 20;   // bytes of a up to which tiles begin at different k
 constexpr int kRaster = 8;        // token tiles of a raster group
 
-// NS stages in LDS, WMW x WNW waves
-template <int TM, int WMW, int WNW, int NS>
+// NSA stages of a and NSB of b in LDS, WMW x WNW waves
+template <int TM, int WMW, int WNW, int NSA, int NSB>
 struct Geom {
   static constexpr int NW = WMW * WNW;
   static constexpr int WM = TM / WMW, WN = kTileN / WNW;   // a wave's tokens, channels
   static constexpr int MI = WM / 32, NI = WN / 32;
-  static constexpr int ABYTES = TM * kTK, STAGE = ABYTES + kTileN * kTK;
-  static constexpr int NA = ABYTES / 1024 / NW, NB = kTileN * kTK / 1024 / NW;   // loads of a wave and stage
+  static constexpr int ABYTES = TM * kTK, BBYTES = kTileN * kTK, BAT = NSA * ABYTES;   // a stage of each; b's ring
+  static constexpr int NA = ABYTES / 1024 / NW, NB = BBYTES / 1024 / NW;   // loads of a wave and stage
   static constexpr int NSC = TM + 2 * kTileN;
   // a wave's store buffer: 32 tokens, or 16 where that is too much, of 64 bytes, padded
-  static constexpr int OROW = 80, OUT = NS * STAGE;
+  static constexpr int OROW = 80, OUT = BAT + NSB * BBYTES;
   static constexpr int OTOK = OUT + NW * 32 * OROW + 2 * NSC * 4 <= 160 * 1024 ? 32 : 16;
   static constexpr int SCALES = OUT + NW * OTOK * OROW;      // fp32 [2][TM + 2 kTileN]: a_scales, b_scales, bias
   static constexpr int LDS = SCALES + 2 * NSC * 4;
   static_assert(LDS <= 160 * 1024, "LDS budget");
-  static_assert(NA * 1024 * NW == ABYTES && NB * 1024 * NW == kTileN * kTK, "whole loads");
+  static_assert(NA * 1024 * NW == ABYTES && NB * 1024 * NW == BBYTES, "whole loads");
 };
 
 // The order of a K-step of P products: after each of the first ones a share of
@@ -58,8 +58,10 @@ __device__ __forceinline__ void wave_lds_order() {
 }
 
 // A persistent workgroup per CU takes its XCD's tiles in turn, their stages as
-// one sequence: the loads run NS stages ahead of the products, across tiles,
-// so the next tile's first stages are on their way while one tile is written.
+// one sequence: the loads run NSA (of a) and NSB (of b) stages ahead of the
+// products, across tiles, so the next tile's first stages are on their way while
+// one tile is written.  b comes from HBM where a single row of tiles covers the
+// tokens, a from the L2: where LDS has room for one stage more it is b's.
 //
 // LDS rows of 128 bytes have their 16-byte units swizzled, so eight rows' reads
 // of one unit fall on eight different bank groups.  A wave reads the operands
@@ -67,10 +69,10 @@ __device__ __forceinline__ void wave_lds_order() {
 // all its reads are done, so there the waves meet, once a stage: the next stage
 // has landed, its first operands are read and later loads overwrite this one,
 // all under the last step's products.
-template <int DT, int TM, int WMW, int WNW, int NS>
+template <int DT, int TM, int WMW, int WNW, int NSA, int NSB>
 __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(WMW * WNW / 4))) void k_i8_tile(
     I8Args g, int m_tiles, int n_tiles, int per_xcd, int turn) {
-  using G = Geom<TM, WMW, WNW, NS>;
+  using G = Geom<TM, WMW, WNW, NSA, NSB>;
   constexpr int MI = G::MI, NI = G::NI;
   extern __shared__ __align__(16) uint8_t i8_lds[];
   lds_u8* const L = (lds_u8*)i8_lds;
@@ -93,73 +95,92 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
     n0 = within / gm * kTileN;
   };
 
-  // ---- loads: the tile and stage they have come to
-  int ld_tile = cur, ld_stage = 0, ld_slot = 0, ld_first = 0;
+  // ---- loads of a and of b: the tile and stage they have come to
+  struct Cursor {
+    int tile, stage, slot, first;   // first: the stage of k that the tile begins with
+  };
+  Cursor ca{cur, 0, 0, 0}, cb{cur, 0, 0, 0};
   __amdgpu_buffer_rsrc_t ra, rb;
   uint32_t ao[G::NA], bo[G::NB];
-  // this lane's unit of its wave's load i: row r, unit p of LDS, holding unit
-  // p ^ swz of the row; rows past the last repeat it
-  auto begin_tile = [&]() {
+  // This lane's unit of its wave's load i: row r, unit p of LDS, holding unit
+  // p ^ swz of the row; rows past the last repeat it.
+  auto unit_of = [&](int i, int n_loads, int& r) {
+    const int off = (wid * n_loads + i) * 1024 + 16 * lane;
+    r = off / kTK;
+    return 16 * ((off % kTK / 16) ^ swz_x(r));
+  };
+  auto begin = [&](auto is_b) {
+    constexpr bool B = decltype(is_b)::value;
+    Cursor& c = B ? cb : ca;
     int m0, n0;
-    tile_at(ld_tile, m0, n0);
-    ld_first = turn ? n0 / kTileN * turn % stages : 0;
-    const int rows = int(g.M - m0 < TM ? g.M - m0 : TM), cols = int(g.N - n0 < kTileN ? g.N - n0 : kTileN);
-    ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.a + m0 * g.lda), 0, (rows - 1) * lda + g.K,
-                                           kBufferWord3);
-    rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.b + n0 * g.ldb), 0, (cols - 1) * ldb + g.K,
-                                           kBufferWord3);
+    tile_at(c.tile, m0, n0);
+    c.first = turn ? n0 / kTileN * turn % stages : 0;
+    const int64_t r0 = B ? n0 : m0, all = B ? g.N : g.M;
+    constexpr int most = B ? kTileN : TM, n_loads = B ? G::NB : G::NA;
+    const int rows = int(all - r0 < most ? all - r0 : most), ld = B ? ldb : lda;
+    (B ? rb : ra) = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(B ? g.b + r0 * g.ldb : g.a + r0 * g.lda), 0,
+                                               (rows - 1) * ld + g.K, kBufferWord3);
 #pragma unroll
-    for (int i = 0; i < G::NA; ++i) {
-      const int off = (wid * G::NA + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-      ao[i] = uint32_t(min(r, rows - 1)) * lda + 16 * (p ^ swz_x(r));
-    }
-#pragma unroll
-    for (int i = 0; i < G::NB; ++i) {
-      const int off = (wid * G::NB + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-      bo[i] = uint32_t(min(r, cols - 1)) * ldb + 16 * (p ^ swz_x(r));
+    for (int i = 0; i < n_loads; ++i) {
+      int r;
+      const int u = unit_of(i, n_loads, r);
+      (B ? bo[i] : ao[i]) = uint32_t(min(r, rows - 1)) * ld + u;
     }
   };
+  using IsA = std::false_type;
+  using IsB = std::true_type;
   auto load = [&](__amdgpu_buffer_rsrc_t r, lds_u8* dst, uint32_t off, int k0) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, reinterpret_cast<__attribute__((address_space(3))) void*>(dst), 16, off,
                                              k0, 0, 0);
   };
-  auto slot_at = [&](int i) { return L + i * G::STAGE; };
-  auto issue_whole = [&]() {
-    lds_u8* const base = slot_at(ld_slot);
-    const int ks = ld_stage + ld_first, k0 = (ks < stages ? ks : ks - stages) * kTK;
-#pragma unroll
-    for (int i = 0; i < G::NA; ++i) load(ra, base + (wid * G::NA + i) * 1024, ao[i], k0);
-#pragma unroll
-    for (int i = 0; i < G::NB; ++i) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], k0);
-    ++ld_stage;
-    ld_slot = ld_slot + 1 == NS ? 0 : ld_slot + 1;
+  auto a_at = [&](int slot) { return L + slot * G::ABYTES; };
+  auto b_at = [&](int slot) { return L + G::BAT + slot * G::BBYTES; };
+  auto k_of = [&](const Cursor& c) {
+    const int ks = c.stage + c.first;
+    return (ks < stages ? ks : ks - stages) * kTK;
   };
-  // the next stage of the sequence, if there is one
-  auto issue_next = [&]() {
-    if (ld_tile >= end) return;
-    const int k0 = ld_stage * kTK;
+  auto pass = [&](Cursor& c, int slots) {
+    ++c.stage;
+    c.slot = c.slot + 1 == slots ? 0 : c.slot + 1;
+  };
+  // a whole stage that is not its tile's last
+  auto issue_whole = [&](auto is_b) {
+    constexpr bool B = decltype(is_b)::value;
+    constexpr int n_loads = B ? G::NB : G::NA;
+    Cursor& c = B ? cb : ca;
+    lds_u8* const to = B ? b_at(c.slot) : a_at(c.slot);
+    const int k0 = k_of(c);
+#pragma unroll
+    for (int i = 0; i < n_loads; ++i)
+      load(B ? rb : ra, to + (wid * n_loads + i) * 1024, B ? bo[i] : ao[i], k0);
+    pass(c, B ? NSB : NSA);
+  };
+  // any next stage of the sequence, if there is one; of the units past K a's are
+  // zeros, b's what is left of an earlier stage
+  auto issue_next = [&](auto is_b) {
+    constexpr bool B = decltype(is_b)::value;
+    Cursor& c = B ? cb : ca;
+    constexpr int n_loads = B ? G::NB : G::NA;
+    if (c.tile >= end) return;
+    lds_u8* const to = B ? b_at(c.slot) : a_at(c.slot);
+    const int k0 = k_of(c);
     if (k0 + kTK <= g.K) {
-      issue_whole();
-    } else {   // the units past K: zeros in a; what is left of an earlier stage in b
-      lds_u8* const base = slot_at(ld_slot);
 #pragma unroll
-      for (int i = 0; i < G::NA; ++i) {
-        const int off = (wid * G::NA + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-        if (k0 + 16 * (p ^ swz_x(r)) < g.K) load(ra, base + (wid * G::NA + i) * 1024, ao[i], k0);
-        else *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(base + off) = u32x4{0, 0, 0, 0};
-      }
+      for (int i = 0; i < n_loads; ++i) load(B ? rb : ra, to + (wid * n_loads + i) * 1024, B ? bo[i] : ao[i], k0);
+    } else {
 #pragma unroll
-      for (int i = 0; i < G::NB; ++i) {
-        const int off = (wid * G::NB + i) * 1024 + 16 * lane, r = off / kTK, p = off % kTK / 16;
-        if (k0 + 16 * (p ^ swz_x(r)) < g.K) load(rb, base + G::ABYTES + (wid * G::NB + i) * 1024, bo[i], k0);
+      for (int i = 0; i < n_loads; ++i) {
+        int r;
+        lds_u8* const at = to + (wid * n_loads + i) * 1024;
+        if (k0 + unit_of(i, n_loads, r) < g.K) load(B ? rb : ra, at, B ? bo[i] : ao[i], k0);
+        else if (!B) *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at + 16 * lane) = u32x4{0, 0, 0, 0};
       }
-      ++ld_stage;
-      ld_slot = ld_slot + 1 == NS ? 0 : ld_slot + 1;
     }
-    if (ld_stage == stages) {
-      ld_stage = 0;
-      ld_tile += step;
-      if (ld_tile < end) begin_tile();
+    pass(c, B ? NSB : NSA);
+    if (c.stage == stages) {
+      c.stage = 0;
+      c.tile += step;
+      if (c.tile < end) begin(is_b);
     }
   };
   // a tile's scales and bias: read into registers, later put into LDS
@@ -188,12 +209,17 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) unit[ks] = uint32_t(lr) * kTK + 16 * ((2 * ks + h) ^ swz_x(lr));
   i32x4 A[2][MI], B[2][NI];
-  auto read = [&](int to, const lds_u8* base, int ks) {
+  int sa_slot = 0, sb_slot = 0;   // of the stage being computed
+  auto read = [&](int to, int ks) {
+    const lds_u8 *const pa = a_at(sa_slot) + unit[ks], *const pb = b_at(sb_slot) + unit[ks];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) A[to][i] = lds_load<i32x4>(base + unit[ks] + (wm * G::WM + 32 * i) * kTK);
+    for (int i = 0; i < MI; ++i) A[to][i] = lds_load<i32x4>(pa + (wm * G::WM + 32 * i) * kTK);
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
-      B[to][i] = lds_load<i32x4>(base + G::ABYTES + unit[ks] + (wn * G::WN + 32 * i) * kTK);
+    for (int i = 0; i < NI; ++i) B[to][i] = lds_load<i32x4>(pb + (wn * G::WN + 32 * i) * kTK);
+  };
+  auto next_stage = [&]() {
+    sa_slot = sa_slot + 1 == NSA ? 0 : sa_slot + 1;
+    sb_slot = sb_slot + 1 == NSB ? 0 : sb_slot + 1;
   };
   i32x16 acc[MI][NI];
   auto multiply = [&](int at) {
@@ -203,31 +229,40 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
       for (int j = 0; j < NI; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(B[at][j], A[at][i], acc[i][j], 0, 0, 0);
   };
-  constexpr int kReads = MI + NI, kLoads = G::NA + G::NB;
-  int slot = 0;   // of the stage being computed
-  auto next_slot = [&]() { return slot + 1 == NS ? 0 : slot + 1; };
+  constexpr int kReads = MI + NI;
+  // Where b runs a stage further ahead than a, its loads are issued a step
+  // later, in the next stage's first.  Loads younger than the next stage's where
+  // the waves meet: those of NSA - 2 stages, or this one's of b.
+  constexpr bool kLateB = NSB > NSA;
+  constexpr int kAhead = kLateB ? G::NB : (NSA - 2) * (G::NA + G::NB);
+  static_assert(NSB == NSA || (NSA == 2 && NSB == 3), "what the counted wait assumes");
   // the steps of a stage but its last
-  auto steps = [&]() {
-    const lds_u8* const base = slot_at(slot);
+  auto steps = [&](auto late_b) {
+    constexpr bool LATE = decltype(late_b)::value;
     __builtin_amdgcn_sched_barrier(0);
-    read(1, base, 1);
+    if constexpr (LATE) issue_whole(IsB{});
+    read(1, 1);
     multiply(0);
-    spread<kReads, 0, MI * NI>();
-    read(0, base, 2);
+    spread<kReads, LATE ? G::NB : 0, MI * NI>();
+    read(0, 2);
     multiply(1);
     spread<kReads, 0, MI * NI>();
-    read(1, base, 3);
+    read(1, 3);
     multiply(0);
     spread<kReads, 0, MI * NI>();
   };
 
-  begin_tile();
+  begin(IsA{});
+  begin(IsB{});
 #pragma unroll
-  for (int i = 0; i < NS; ++i) issue_next();
+  for (int i = 0; i < NSA; ++i) {   // (of b one more, where there is room, in the first stage)
+    issue_next(IsA{});
+    issue_next(IsB{});
+  }
   fetch_scales(cur);
   put_scales(0);
   wait_loads_barrier<0>();
-  read(0, slot_at(0), 0);
+  read(0, 0);
   int half = 0;
   for (; cur < end; cur += step, half ^= 1) {
 #pragma unroll
@@ -238,25 +273,28 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
     if (cur + step < end) fetch_scales(cur + step);
     int s = 0;
-    const int full = stages - 1 - NS;   // stages whose load is of this tile, and not its last: whole
+    const int full = stages - 1 - NSA;   // stages whose loads are of this tile, and not its last: whole
 #pragma unroll 1
     for (; s < full; ++s) {
-      steps();
-      wait_loads_barrier<(NS - 2) * kLoads>();
+      steps(std::integral_constant<bool, kLateB>{});
+      wait_loads_barrier<kAhead>();
       __builtin_amdgcn_sched_barrier(0);
-      issue_whole();
-      slot = next_slot();
-      read(0, slot_at(slot), 0);
+      issue_whole(IsA{});
+      if constexpr (!kLateB) issue_whole(IsB{});
+      next_stage();
+      read(0, 0);
       multiply(1);
-      spread<kReads, kLoads, MI * NI>();
+      spread<kReads, G::NA + (kLateB ? 0 : G::NB), MI * NI>();
     }
 #pragma unroll 1
     for (; s < stages; ++s) {
-      steps();
+      if constexpr (kLateB) issue_next(IsB{});
+      steps(std::false_type{});
       wait_loads_barrier<0>();
-      issue_next();
-      slot = next_slot();
-      read(0, slot_at(slot), 0);   // (behind the last stage: values that nothing uses)
+      issue_next(IsA{});
+      if constexpr (!kLateB) issue_next(IsB{});
+      next_stage();
+      read(0, 0);   // (behind the last stage: values that nothing uses)
       multiply(1);
     }
     put_scales(half ^ 1);   // (read in the epilogue before this one, by waves that have met since)
@@ -312,9 +350,9 @@ __global__ __launch_bounds__(WMW* WNW * 64) __attribute__((amdgpu_waves_per_eu(W
   }
 }
 
-template <int DT, int TM, int WMW, int WNW, int NS>
+template <int DT, int TM, int WMW, int WNW, int NSA, int NSB>
 hipError_t launch(const I8Args& g, int n_cu, hipStream_t s) {
-  using G = Geom<TM, WMW, WNW, NS>;
+  using G = Geom<TM, WMW, WNW, NSA, NSB>;
   const int m_tiles = int((g.M + TM - 1) / TM), n_tiles = int((g.N + kTileN - 1) / kTileN);
   const int per_xcd = (m_tiles * n_tiles + 7) / 8, wgs = 8 * std::min(per_xcd, std::max(n_cu / 8, 1));
   // Tiles of neighbouring channels begin at different k (the sums are exact in
@@ -322,7 +360,7 @@ hipError_t launch(const I8Args& g, int n_cu, hipStream_t s) {
   // two all ask for the same memory channels at once (64 x 151936 x 4096:
   // 158 -> 127 us).
   const int turn = g.K % kTK == 0 && g.M * g.K <= kTurnMost ? 5 : 0;
-  return launch_kernel_lds(k_i8_tile<DT, TM, WMW, WNW, NS>, dim3(unsigned(wgs)), dim3(G::NW * 64), G::LDS, s, g, m_tiles,
+  return launch_kernel_lds(k_i8_tile<DT, TM, WMW, WNW, NSA, NSB>, dim3(unsigned(wgs)), dim3(G::NW * 64), G::LDS, s, g, m_tiles,
                            n_tiles, per_xcd, turn);
 }
 
@@ -352,10 +390,13 @@ hipError_t launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
       best = cost;
     }
   }
-  return tm == 256   ? launch<DT, 256, 2, 4, 2>(g, n_cu, s)
-         : tm == 192 ? launch<DT, 192, 2, 4, 2>(g, n_cu, s)
-         : tm == 128 ? launch<DT, 128, 2, 4, 3>(g, n_cu, s)
-                     : launch<DT, 64, 1, 8, 3>(g, n_cu, s);
+#ifdef I8TM
+  return launch<DT, I8TM>(g, n_cu, s);
+#endif
+  return tm == 256   ? launch<DT, 256, 2, 4, 2, 2>(g, n_cu, s)
+         : tm == 192 ? launch<DT, 192, 2, 4, 2, 3>(g, n_cu, s)
+         : tm == 128 ? launch<DT, 128, 2, 4, 3, 3>(g, n_cu, s)
+                     : launch<DT, 64, 1, 8, 3, 3>(g, n_cu, s);
 }
 template hipError_t launch_tiles<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
 template hipError_t launch_tiles<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
