@@ -7,7 +7,7 @@ namespace archead {
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
-constexpr int kBeamChunk = 512;    // logits of a chunk
+constexpr int kBeamChunk = 128;    // logits of a chunk, the least
 constexpr int kBeamSpan = 2048;    // logits of a span, a wave's share of a row
 
 // of a span of a row: sum of exp(logit - top); top is its largest logit, or 0

@@ -17,10 +17,16 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // sum of exponentials).  k_beam_pick, a workgroup per sequence, makes the rows'
 // logsumexp of them and with it the chunks' largest scores.  If n chunks are
 // ranked by (largest score, then position), every pair among the n best lies in
-// one of the first n, so the logits of no more than those are read again.
+// one of the first n, so the logits of few more than those are read again.
+// FINE: chunks of 128 logits (16 lanes' eight) instead of 512 (a wave's): fewer
+// pairs above the floor that the chunks' maxima give, but four times as many
+// chunks to look at.
 constexpr int kScanBlock = 256;
-constexpr int kSpanChunks = archead::kBeamSpan / archead::kBeamChunk;
-static_assert(archead::kBeamChunk == 64 * 8, "a wave takes a chunk per step");
+constexpr int kSteps = archead::kBeamSpan / 512;   // a wave's loads of a span
+__host__ __device__ constexpr int chunk_lanes(bool fine) { return fine ? 16 : 64; }
+__host__ __device__ constexpr int chunk_logits(bool fine) { return 8 * chunk_lanes(fine); }
+__host__ __device__ constexpr int span_chunks(bool fine) { return archead::kBeamSpan / chunk_logits(fine); }
+static_assert(chunk_logits(true) == archead::kBeamChunk, "the workspace holds the smaller chunks' maxima");
 
 // fp64 values as integers of the same order; 0 for -inf and NaN
 __device__ __forceinline__ uint64_t order_key(double v) {
@@ -36,10 +42,10 @@ constexpr uint32_t neg_inf() {
 struct ScanArgs {
   const uint8_t* logits;
   int64_t V, row_bytes;
-  int64_t n_span;          // spans of a row; kSpanChunks times as many chunks
+  int64_t n_span;            // spans of a row
   const float* scores;
   const uint8_t* finished;   // may be null
-  float* cmax;               // [rows][n_span * kSpanChunks]
+  float* cmax;               // [rows][n_span][chunks of a span]
   archead::BeamSpanSum* span;   // [rows][n_span]
 };
 
@@ -56,13 +62,16 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_f(float v) {
   return __uint_as_float(dpp_u<CTRL>(__float_as_uint(v)));
 }
-__device__ __forceinline__ float wave_max(float v) {
+__device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, dpp_f<0xB1>(v));
   v = fmaxf(v, dpp_f<0x4E>(v));
   v = fmaxf(v, dpp_f<0x141>(v));
-  v = fmaxf(v, dpp_f<0x140>(v));
+  return fmaxf(v, dpp_f<0x140>(v));
+}
+__device__ __forceinline__ float rows_max(float v) {
   return fmaxf(fmaxf(lane_f(v, 0), lane_f(v, 16)), fmaxf(lane_f(v, 32), lane_f(v, 48)));
 }
+__device__ __forceinline__ float wave_max(float v) { return rows_max(row_max(v)); }
 __device__ __forceinline__ double of_words(uint32_t lo, uint32_t hi) {
   return __longlong_as_double((long long)(uint64_t(hi) << 32 | lo));
 }
@@ -89,58 +98,64 @@ __device__ __forceinline__ bool row_counts(const ScanArgs& a, int64_t r) {
   return fabsf(a.scores[r]) < INFINITY && !(a.finished && a.finished[r]);
 }
 
-// Span sp of row r, by a wave: its chunks' largest logits to cmax[0 ..
-// kSpanChunks), its sum of exponentials to *span.
-template <int DT>
+// Span sp of row r, by a wave: its chunks' largest logits to cmax, its sum of
+// exponentials to *span.
+template <int DT, bool FINE>
 __device__ __forceinline__ void scan_span(const ScanArgs& a, int64_t r, int64_t sp, int lane, float* cmax,
                                           archead::BeamSpanSum* span) {
   const uint8_t* row = a.logits + r * a.row_bytes;
-  Eight<DT> e[kSpanChunks];
+  Eight<DT> e[kSteps];
 #pragma unroll
-  for (int c = 0; c < kSpanChunks; ++c)
-    e[c].load(row, sp * archead::kBeamSpan + c * archead::kBeamChunk + lane * 8, a.V, neg_inf<DT>());
-  float cm[kSpanChunks], top = -INFINITY;
+  for (int c = 0; c < kSteps; ++c)
+    e[c].load(row, sp * archead::kBeamSpan + c * 512 + lane * 8, a.V, neg_inf<DT>());
+  float cm[kSteps], top = -INFINITY;   // cm: of 16 lanes
 #pragma unroll
-  for (int c = 0; c < kSpanChunks; ++c) {
+  for (int c = 0; c < kSteps; ++c) {
     float m = e[c].at(0);
 #pragma unroll
     for (int i = 1; i < 8; ++i) m = fmaxf(m, e[c].at(i));
-    cm[c] = wave_max(m);
+    cm[c] = row_max(m);
+    if constexpr (!FINE) cm[c] = rows_max(cm[c]);
     top = fmaxf(top, cm[c]);
   }
+  if constexpr (FINE) top = rows_max(top);
   // relative to 0 where nothing is above -inf: every term is then 0, or NaN
   const float ref = top > -INFINITY ? top : 0.f;
   float s = 0.f;
 #pragma unroll
-  for (int c = 0; c < kSpanChunks; ++c)
+  for (int c = 0; c < kSteps; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f((e[c].at(i) - ref) * 1.4426950408889634f);
   const double sd = wave_sum(double(s));
   if (lane == 0) *span = archead::BeamSpanSum{sd, ref};
-  if (lane < kSpanChunks) {
+  const int c = lane & 15;   // lane c of a row of 16 writes its maximum of step c
+  if (c < kSteps && (FINE || lane < 16)) {
     float m = cm[0];
 #pragma unroll
-    for (int c = 1; c < kSpanChunks; ++c) m = lane == c ? cm[c] : m;
-    cmax[lane] = m;
+    for (int i = 1; i < kSteps; ++i) m = c == i ? cm[i] : m;
+    cmax[FINE ? 4 * c + (lane >> 4) : c] = m;
   }
 }
 
-template <int DT>
+template <int DT, bool FINE>
 __global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
   const int lane = threadIdx.x & 63;
   const int wid = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int64_t r = blockIdx.y, sp = int64_t(blockIdx.x) * (kScanBlock / 64) + wid;
   if (sp >= a.n_span || !row_counts(a, r)) return;
   const int64_t i = r * a.n_span + sp;
-  scan_span<DT>(a, r, sp, lane, a.cmax + i * kSpanChunks, a.span + i);
+  scan_span<DT, FINE>(a, r, sp, lane, a.cmax + i * span_chunks(FINE), a.span + i);
 }
 
 constexpr int kPickBlock = 1024, kPickWaves = kPickBlock / 64;
 constexpr int kPickHeld = 4;     // chunks whose largest logits a thread keeps
+constexpr int kPickAhead = 2;    // listed chunks that a thread reads of at a time
 constexpr int kPickSpans = 4;    // spans whose sums a lane keeps
 constexpr int kPickGroups = kPickBlock / 16;   // groups of threads that share a maximum
 constexpr int kPickList = 512;   // chunks, and pairs, that are ranked one against all
 static_assert(kPickList >= archead::kTopKMaxK + ARCHEAD_BEAM_MAX, "room for the n best and the ended beams");
+constexpr int kFineMost = 64;    // spans of a sequence up to which the chunks are the smaller ones
+constexpr int kPickRank = 96;    // pairs up to which no second floor is looked for
 static_assert(kPickGroups == 64, "a lane of a wave for each");
 
 struct PickArgs {
@@ -163,9 +178,9 @@ __device__ __forceinline__ bool before(double sa, uint64_t ia, double sb, uint64
 
 // FEW: no more spans in a sequence than waves, which read them here (no first
 // launch)
-template <int DT, bool FEW>
+template <int DT, bool FINE, bool FEW>
 __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
-  __shared__ float few_cmax[FEW ? kPickWaves * kSpanChunks : 1];
+  __shared__ float few_cmax[FEW ? kPickWaves * span_chunks(FINE) : 1];
   __shared__ archead::BeamSpanSum few_span[FEW ? kPickWaves : 1];
   __shared__ double lse[ARCHEAD_BEAM_MAX], cum[ARCHEAD_BEAM_MAX];   // lse: NaN where a row offers nothing by its logits
   __shared__ bool ended[ARCHEAD_BEAM_MAX];
@@ -179,17 +194,19 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t b = blockIdx.x, r0 = b * p.K;
-  const int n_span = int(a.n_span), n_chunk = n_span * kSpanChunks, n_items = n_chunk * p.K;   // (K V / 512 < 2^27)
+  const int n_span = int(a.n_span), stored = n_span * span_chunks(FINE);   // a row's maxima in memory
+  const int n_chunk = int((a.V + chunk_logits(FINE) - 1) / chunk_logits(FINE)), n_items = n_chunk * p.K;   // (K V / 512 < 2^27)
   if (tid == 0) n_list = n_pair = 0;
   if constexpr (FEW) {
     const int k = wid / n_span;
     if (k < p.K && row_counts(a, r0 + k))
-      scan_span<DT>(a, r0 + k, wid - k * n_span, lane, few_cmax + wid * kSpanChunks, few_span + wid);
+      scan_span<DT, FINE>(a, r0 + k, wid - k * n_span, lane, few_cmax + wid * span_chunks(FINE), few_span + wid);
     __syncthreads();
   }
   auto cmax_of = [&](int item) {
-    if constexpr (FEW) return few_cmax[item];
-    else return a.cmax[r0 * n_chunk + item];
+    const int k = item / n_chunk, c = item - k * n_chunk;
+    if constexpr (FEW) return few_cmax[k * stored + c];
+    else return a.cmax[(r0 + k) * stored + c];
   };
   auto span_of = [&](int k, int i) {
     if constexpr (FEW) return few_span[k * n_span + i];
@@ -354,25 +371,27 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   // ---- the pairs at or above the floor, and the ended beams'
   auto offers_end = [&](int k) { return k < p.K && ended[k] && fabs(cum[k]) < INFINITY; };
   auto pair = [&](int k, int64_t v) { return uint64_t(k) << 32 | uint64_t(v); };
+  constexpr int kLanes = chunk_lanes(FINE), kAtOnce = kPickBlock / kLanes;   // chunks that the workgroup reads at once
+  const int eight = tid % kLanes * 8;
   auto fetch = [&](Eight<DT>& e, int c) {   // this lane's eight logits of listed chunk c
     const int item = chunks[c], k = item / n_chunk;
-    e.load(a.logits + (r0 + k) * a.row_bytes, int64_t(item - k * n_chunk) * archead::kBeamChunk + lane * 8, a.V,
-           neg_inf<DT>());
+    e.load(a.logits + (r0 + k) * a.row_bytes, int64_t(item - k * n_chunk) * chunk_logits(FINE) + eight, a.V, neg_inf<DT>());
   };
   auto each = [&](const Eight<DT>& e, int c, auto use) {   // use(score, pair) for them
     const int item = chunks[c], k = item / n_chunk;
-    const int64_t v0 = int64_t(item - k * n_chunk) * archead::kBeamChunk + lane * 8;
+    const int64_t v0 = int64_t(item - k * n_chunk) * chunk_logits(FINE) + eight;
 #pragma unroll
     for (int i = 0; i < 8; ++i) use(score_of(k, e.at(i)), pair(k, v0 + i));
   };
-  auto each_logit = [&](auto use) {   // of the wave's chunks, two of them read at a time
-    for (int c = wid; c < n_ch; c += 2 * kPickWaves) {
-      Eight<DT> e0, e1;
-      const bool two = c + kPickWaves < n_ch;
-      fetch(e0, c);
-      if (two) fetch(e1, c + kPickWaves);
-      each(e0, c, use);
-      if (two) each(e1, c + kPickWaves, use);
+  auto each_logit = [&](auto use) {   // of the listed chunks
+    for (int c0 = tid / kLanes; c0 < n_ch; c0 += kPickAhead * kAtOnce) {
+      Eight<DT> e[kPickAhead];
+#pragma unroll
+      for (int u = 0; u < kPickAhead; ++u)
+        if (c0 + u * kAtOnce < n_ch) fetch(e[u], c0 + u * kAtOnce);
+#pragma unroll
+      for (int u = 0; u < kPickAhead; ++u)
+        if (c0 + u * kAtOnce < n_ch) each(e[u], c0 + u * kAtOnce, use);
     }
   };
   auto put = [&](double s, uint64_t i) {
@@ -385,41 +404,59 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
     return f > 1 ? __longlong_as_double((long long)(k >> 63 ? k ^ (uint64_t(1) << 63) : ~k)) : -DBL_MAX;
   };
   const double least = score_at(floor);
-  if (offers_end(tid)) put(cum[tid], pair(tid, p.end_token));
+  double top = -INFINITY;   // this lane's best pair
+  if (offers_end(tid)) {
+    top = cum[tid];
+    put(cum[tid], pair(tid, p.end_token));
+  }
   each_logit([&](double s, uint64_t i) {
-    if (s >= least) put(s, i);
+    if (s >= least) {
+      top = fmax(top, s);
+      put(s, i);
+    }
   });
   __syncthreads();
   int np = n_pair;
-  if (__builtin_expect(np > kPickList, 0)) {
-    // Too many (few chunks, or the best logits side by side): a second floor,
-    // about the n-th largest of the lanes' best pairs, and those that reach it.
-    uint32_t top = offers_end(tid) ? uint32_t(order_key(cum[tid]) >> 32) : 0u;
-    each_logit([&](double s, uint64_t) { top = max(top, uint32_t(order_key(s) >> 32)); });
-    lane_key[tid] = top;
+  if (np > kPickRank) {
+    // More than are ranked quickly (beams of unlike scores, few chunks, the best
+    // logits side by side): a second floor, about the n-th largest of those
+    // listed, or of the lanes' best where they are too many to list.
+    const bool listed = np <= kPickList;
+    Ranked r{-INFINITY, 0};
+    if (listed && tid < np) r = list[tid];
+    lane_key[tid] = uint32_t(order_key(listed ? r.score : top) >> 32);
     __syncthreads();
-    if (tid == 0) n_pair = 0;
-    uint32_t kk[kPickWaves];
+    if (wid == 0) {
+      if (lane == 0) n_pair = 0;
+      const int regs = listed ? kPickList / 64 : kPickWaves;
+      uint32_t kk[kPickWaves];
 #pragma unroll
-    for (int i = 0; i < kPickWaves; ++i) kk[i] = lane_key[64 * i + lane];
-    uint32_t f = 0;
-    int reach = kPickBlock;
-    for (int bit = 31; bit >= 0 && reach > p.n + p.n / 4; --bit) {
-      const uint32_t t = f | (1u << bit);
-      int c = 0;
+      for (int i = 0; i < kPickWaves; ++i) kk[i] = i < regs ? lane_key[64 * i + lane] : 0u;
+      uint32_t f = 0;
+      int reach = kPickBlock;
+      for (int bit = 31; bit >= 0 && reach > p.n + p.n / 4; --bit) {
+        const uint32_t t = f | (1u << bit);
+        int c = 0;
 #pragma unroll
-      for (int i = 0; i < kPickWaves; ++i) c += __popcll(__ballot(kk[i] >= t));
-      if (c >= p.n) {
-        f = t;
-        reach = c;
+        for (int i = 0; i < kPickWaves; ++i)
+          if (i < regs) c += __popcll(__ballot(kk[i] >= t));
+        if (c >= p.n) {
+          f = t;
+          reach = c;
+        }
       }
+      if (lane == 0) skey[0] = max(f, 1u);
     }
-    const double least2 = score_at(max(f, 1u));
     __syncthreads();
-    if (offers_end(tid) && cum[tid] >= least2) put(cum[tid], pair(tid, p.end_token));
-    each_logit([&](double s, uint64_t i) {
-      if (s >= least2) put(s, i);
-    });
+    const double least2 = score_at(skey[0]);
+    if (listed) {
+      if (tid < np && r.score >= least2) put(r.score, r.at);
+    } else {
+      if (offers_end(tid) && cum[tid] >= least2) put(cum[tid], pair(tid, p.end_token));
+      each_logit([&](double s, uint64_t i) {
+        if (s >= least2) put(s, i);
+      });
+    }
     __syncthreads();
     np = n_pair;
   }
@@ -481,16 +518,23 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   }
 }
 
+template <int DT, bool FINE>
+hipError_t launch_select_as(const PickArgs& p, int64_t B, hipStream_t s) {
+  const dim3 grid{unsigned((p.in.n_span + kScanBlock / 64 - 1) / (kScanBlock / 64)), unsigned(B * p.K)};
+  const hipError_t e = launch_kernel(k_beam_scan<DT, FINE>, grid, dim3(kScanBlock), 0, s, p.in);
+  if (e != hipSuccess) return e;
+  return launch_kernel(k_beam_pick<DT, FINE, false>, dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
+}
+
 template <int DT>
 hipError_t launch_select(const PickArgs& p, int64_t B, hipStream_t s) {
   // One launch where every wave has at most one span of a sequence (GPU time is
   // the same, a launch takes the host 3 us).
   if (p.in.n_span * p.K <= kPickWaves)
-    return launch_kernel(k_beam_pick<DT, true>, dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
-  const dim3 grid{unsigned((p.in.n_span + kScanBlock / 64 - 1) / (kScanBlock / 64)), unsigned(B * p.K)};
-  const hipError_t e = launch_kernel(k_beam_scan<DT>, grid, dim3(kScanBlock), 0, s, p.in);
-  if (e != hipSuccess) return e;
-  return launch_kernel(k_beam_pick<DT, false>, dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
+    return launch_kernel(k_beam_pick<DT, true, true>, dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
+  // us with chunks of 128 / 512: 12 x 16 beams over 4320 tokens 11.6 / 25, 4 over
+  // 32000 (64 spans) 8.6 / 9.3, over 50257 (100) 9.2 / 8.6, 8 x 4 over 151936 15.3 / 13.1.
+  return p.in.n_span * p.K <= kFineMost ? launch_select_as<DT, true>(p, B, s) : launch_select_as<DT, false>(p, B, s);
 }
 
 // ------------------------------------------------------------- reordering
