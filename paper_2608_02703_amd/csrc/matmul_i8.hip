@@ -9,65 +9,96 @@ namespace {
 using namespace archead::i8;
 
 // ---------------------------------------------- any alignment, any K
-// Tiles of 64 tokens x 64 channels, 128 of k at a time through registers into
-// LDS, bytes past K as zeros.  Four waves of 32 x 32.
-constexpr int kABlock = 256, kATile = 64, kAK = 128, kAStride = kAK + 16;
+// Tiles of T tokens x T channels, 128 k a stage, bytes past K as zeros, four
+// waves of T/2 x T/2.  Rows that begin at any byte cannot be loaded to LDS
+// directly: each thread loads its pieces of the next stage into registers while
+// the waves multiply this one, and puts them into the other half of LDS after.
+constexpr int kABlock = 256, kAK = 128, kARow = kAK + 16;   // (rows padded: no bank is hit twice as often)
 
-template <int DT>
+template <int DT, int T>
 __global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, int64_t tiles) {
-  __shared__ __align__(16) int8_t lds[2][kATile * kAStride];
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-  const int wm = (wid & 1) * 32, wn = (wid >> 1) * 32;
+  constexpr int F = T / 32, NP = T * 8 / kABlock;   // fragments of 16 rows a wave, pieces of 16 bytes a thread
+  __shared__ __align__(16) int8_t la[2][T * kARow], lb[2][T * kARow];
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q = lane >> 4;
+  const int wid = tid >> 6, wm = (wid & 1) * (T / 2), wn = (wid >> 1) * (T / 2);
   for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t m0 = (t % m_tiles) * kATile, n0 = (t / m_tiles) * kATile;
-    i32x4 acc[2][2] = {};
-    for (int k0 = 0; k0 < g.K; k0 += kAK) {
-      uint4 w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {   // two pieces of a's tile, two of b's
-        const int piece = tid + (i & 1) * kABlock, row = piece / 8, k = k0 + (piece % 8) * 16;
-        const int64_t r = (i < 2 ? m0 : n0) + row;
-        const int8_t* p = i < 2 ? g.a + r * g.lda + k : g.b + r * g.ldb + k;
-        w[i] = uint4{0, 0, 0, 0};
-        if (r < (i < 2 ? g.M : g.N)) {
-          if (k + 16 <= g.K) w[i] = load_any<uint4>(p);
-          else {
-            uint32_t d[4] = {};
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (k + j < g.K) d[j / 4] |= uint32_t(uint8_t(p[j])) << (8 * (j % 4));
-            w[i] = uint4{d[0], d[1], d[2], d[3]};
-          }
-        }
+    const int64_t m0 = t % m_tiles * T, n0 = t / m_tiles * T;
+    uint4 wa[NP], wb[NP];
+    auto piece = [&](const int8_t* base, int64_t r, int64_t rows, int64_t ld, int k) {
+      uint4 w{0, 0, 0, 0};
+      if (r >= rows || k >= g.K) return w;
+      const int8_t* const row = base + r * ld;
+      if (__builtin_expect(g.K < 16, 0)) {
+        uint32_t d[4] = {};
+        for (int j = 0; j < g.K; ++j) d[j / 4] |= uint32_t(uint8_t(row[j])) << (8 * (j % 4));
+        return uint4{d[0], d[1], d[2], d[3]};
       }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int piece = tid + (i & 1) * kABlock;
-        *reinterpret_cast<uint4*>(&lds[i / 2][(piece / 8) * kAStride + (piece % 8) * 16]) = w[i];
+      // the row's last 16 bytes, moved down, where fewer are left
+      const int over = max(k + 16 - g.K, 0);
+      w = load_any<uint4>(row + k - over);
+      if (over) {
+        uint64_t lo = uint64_t(w.y) << 32 | w.x, hi = uint64_t(w.w) << 32 | w.z;
+        const int bits = 8 * over;
+        lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+        hi = bits < 64 ? hi >> bits : 0;
+        w = uint4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
       }
-      __syncthreads();
+      return w;
+    };
+    auto fetch = [&](int k0) {
+      const int k = k0 + tid % 8 * 16;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        wa[i] = piece(g.a, m0 + tid / 8 + 32 * i, g.M, g.lda, k);
+        wb[i] = piece(g.b, n0 + tid / 8 + 32 * i, g.N, g.ldb, k);
+      }
+    };
+    auto put = [&](int half) {
+      const int at = tid / 8 * kARow + tid % 8 * 16;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        *reinterpret_cast<uint4*>(&la[half][at + 32 * i * kARow]) = wa[i];
+        *reinterpret_cast<uint4*>(&lb[half][at + 32 * i * kARow]) = wb[i];
+      }
+    };
+    i32x4 acc[F][F] = {};
+    fetch(0);
+    __syncthreads();   // the tile before this one has been read
+    put(0);
+    __syncthreads();
+    int half = 0;
+    for (int k0 = 0; k0 < g.K; k0 += kAK, half ^= 1) {
+      const bool more = k0 + kAK < g.K;
+      if (more) fetch(k0 + kAK);
 #pragma unroll
       for (int kk = 0; kk < kAK; kk += 64) {
-        i32x4 fa[2], fb[2];
+        i32x4 fa[F], fb[F];
+        const int at = lr * kARow + kk + 16 * q;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int at = (lane & 15) * kAStride + kk + (lane >> 4) * 16;
-          fa[i] = *reinterpret_cast<const i32x4*>(&lds[0][(wm + 16 * i) * kAStride + at]);
-          fb[i] = *reinterpret_cast<const i32x4*>(&lds[1][(wn + 16 * i) * kAStride + at]);
+        for (int i = 0; i < F; ++i) {
+          fa[i] = *reinterpret_cast<const i32x4*>(&la[half][(wm + 16 * i) * kARow + at]);
+          fb[i] = *reinterpret_cast<const i32x4*>(&lb[half][(wn + 16 * i) * kARow + at]);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < F; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
       }
+      if (more) put(half ^ 1);   // (read last in the stage before, behind a meeting)
+      __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < F; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        finish4<DT>(g, m0 + wm + 16 * i + (lane & 15), n0 + wn + 16 * j + 4 * (lane >> 4), acc[i][j]);
+      for (int j = 0; j < F; ++j) finish4<DT>(g, m0 + wm + 16 * i + lr, n0 + wn + 16 * j + 4 * q, acc[i][j]);
   }
+}
+
+template <int DT, int T>
+hipError_t launch_any(const I8Args& g, hipStream_t s) {
+  const int64_t mt = (g.M + T - 1) / T, tiles = mt * ((g.N + T - 1) / T);
+  return launch_kernel(k_i8_any<DT, T>, dim3(unsigned(tiles < (1 << 22) ? tiles : 1 << 22)), dim3(kABlock), 0, s, g, mt,
+                       tiles);
 }
 
 // compute units of the current device, asked for once
@@ -94,9 +125,10 @@ hipError_t launch_matmul(const I8Args& g, hipStream_t s) {
     if (few) return launch_few<DT>(g, n_cu, s);
     if (tiles_take(g)) return launch_tiles<DT>(g, n_cu, s);
   }
-  const int64_t mt = (g.M + kATile - 1) / kATile, nt = (g.N + kATile - 1) / kATile, tiles = mt * nt;
-  const dim3 grid{unsigned(tiles < (1 << 22) ? tiles : 1 << 22)};
-  return launch_kernel(k_i8_any<DT>, grid, dim3(kABlock), 0, s, g, mt, tiles);
+  // us with 128 / 64: 1172 x 43472 x 4229 451 / 727, 200 x 30000 x 1001 25 / 36,
+  // 4096 x 4096 x 4095 116 / 203, but 3127 x 3460 x 141 25 / 21.
+  const int64_t large = ((g.M + 127) / 128) * ((g.N + 127) / 128);
+  return large >= 400 && g.K > 2 * kAK ? launch_any<DT, 128>(g, s) : launch_any<DT, 64>(g, s);
 }
 
 }  // namespace
