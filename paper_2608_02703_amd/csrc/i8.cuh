@@ -75,7 +75,7 @@ __device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, c
     const int64_t c = n + i < g.N ? n + i : n;
     y[i] = scaled(acc[i], s, g.sb[c], g.bias ? g.bias[c] : 0.f);
   }
-  uint32_t w[EB];
+  alignas(16) uint32_t w[EB];
   put4<DT>(reinterpret_cast<uint8_t*>(w), y);
   if constexpr (EB == 4) store_part<EB>(g.out + (m * g.ldo + n) * EB, uint4{w[0], w[1], w[2], w[3]}, g.N - n);
   else store_part<EB>(g.out + (m * g.ldo + n) * EB, uint2{w[0], w[1]}, g.N - n);
