@@ -133,10 +133,10 @@ template <int DT>
 hipError_t launch_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes, int8_t* codes, int64_t ldc,
                      float* scales, hipStream_t s) {
   // Fewer waves with more in flight each where there are plenty: us with 2 / 4
-  // groups 151936 x 4096 336 / 312, 16384 x 8192 88 / 74, 4096 x 4096 12.7 / 13.3,
-  // 300 x 4096 4.5 / 5.8.
+  // groups 151936 x 4096 336 / 312, 16384 x 8192 88 / 74, 14709 x 4128 45 / 38,
+  // 8192 x 4096 20.5 / 21.7, 4096 x 4096 12.2 / 13.1, 300 x 4096 4.5 / 5.8.
   if (d <= kQShort) return launch_rows<DT, true, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
-  if (M * d < (1 << 26)) return launch_rows<DT, false, 2>(x, M, d, row_bytes, codes, ldc, scales, s);
+  if (M * d < (1 << 25)) return launch_rows<DT, false, 2>(x, M, d, row_bytes, codes, ldc, scales, s);
   return launch_rows<DT, false, 4>(x, M, d, row_bytes, codes, ldc, scales, s);
 }
 
