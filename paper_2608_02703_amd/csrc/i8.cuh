@@ -81,6 +81,13 @@ __device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, c
   else store_part<EB>(g.out + (m * g.ldo + n) * EB, uint2{w[0], w[1]}, g.N - n);
 }
 
+// LDS accesses of one wave stay in this order (the hardware keeps it; lanes
+// read what other lanes wrote, which the compiler does not see).
+__device__ __forceinline__ void wave_lds_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
 constexpr int64_t kMaxLd = 1 << 22;   // a tile's rows stay within 31-bit offsets
 
 // What the kernels below need: 16-byte pieces that lie whole in a row and in
@@ -92,9 +99,12 @@ inline bool pieces(const I8Args& g) {
 bool few_take(const I8Args& g);
 template <int DT>
 hipError_t launch_few(const I8Args& g, int n_cu, hipStream_t s);
+bool split_take(const I8Args& g);
+template <int DT>   // in tiles of 16 f x 16 f, f = 1 or 2
+hipError_t launch_split(const I8Args& g, int f, hipStream_t s);
 bool tiles_take(const I8Args& g);
-template <int DT>
-hipError_t launch_tiles(const I8Args& g, int n_cu, hipStream_t s);
+template <int DT>   // in tiles of tm x 256, tm = 64, 128, 192 or 256
+hipError_t launch_tiles(const I8Args& g, int tm, int n_cu, hipStream_t s);
 
 }  // namespace i8
 }  // namespace archead

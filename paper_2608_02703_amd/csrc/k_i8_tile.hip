@@ -50,13 +50,6 @@ __device__ __forceinline__ void spread() {
   }
 }
 
-// LDS accesses of one wave stay in this order (the hardware keeps it; lanes
-// read what other lanes wrote, which the compiler does not see).
-__device__ __forceinline__ void wave_lds_order() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // A persistent workgroup per CU takes its XCD's tiles in turn, their stages as
 // one sequence: the loads run NSA (of a) and NSB (of b) stages ahead of the
 // products, across tiles, so the next tile's first stages are on their way while
@@ -375,29 +368,15 @@ bool tiles_take(const I8Args& g) {
 }
 
 template <int DT>
-hipError_t launch_tiles(const I8Args& g, int n_cu, hipStream_t s) {
-  // The height for which the CUs' rounds of tiles load the fewest bytes, what
-  // bounds a stage but for the tallest: us at 64 / 128 / 192 / 256 rows for M x N x K
-  // 64 x 151936 x 4096 127 / 140 / - / 167, 333 x 50257 x 1536 63 / 53 / 48 / 51,
-  // 512 x 128256 x 8192 795 / 548 / 576 / 485, 256 x 8192 x 4096 19 / - / - / 41.
-  int tm = 0;
-  int64_t best = 0;
-  for (int t : {256, 192, 128, 64}) {
-    const int64_t tiles = (g.M + t - 1) / t * ((g.N + kTileN - 1) / kTileN);
-    const int64_t cost = (tiles + n_cu - 1) / n_cu * (t + kTileN);
-    if (!tm || cost < best) {
-      tm = t;
-      best = cost;
-    }
-  }
+hipError_t launch_tiles(const I8Args& g, int tm, int n_cu, hipStream_t s) {
   return tm == 256   ? launch<DT, 256, 2, 4, 2, 2>(g, n_cu, s)
          : tm == 192 ? launch<DT, 192, 2, 4, 2, 3>(g, n_cu, s)
          : tm == 128 ? launch<DT, 128, 2, 4, 3, 3>(g, n_cu, s)
                      : launch<DT, 64, 1, 8, 3, 3>(g, n_cu, s);
 }
-template hipError_t launch_tiles<ARCHEAD_F32>(const I8Args&, int, hipStream_t);
-template hipError_t launch_tiles<ARCHEAD_BF16>(const I8Args&, int, hipStream_t);
-template hipError_t launch_tiles<ARCHEAD_F16>(const I8Args&, int, hipStream_t);
+template hipError_t launch_tiles<ARCHEAD_F32>(const I8Args&, int, int, hipStream_t);
+template hipError_t launch_tiles<ARCHEAD_BF16>(const I8Args&, int, int, hipStream_t);
+template hipError_t launch_tiles<ARCHEAD_F16>(const I8Args&, int, int, hipStream_t);
 
 }  // namespace i8
 }  // namespace archead

@@ -63,6 +63,15 @@ __global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, i
     };
     i32x4 acc[F][F] = {};
     fetch(0);
+    f32x4v sb[F], bi[F];
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t n = n0 + wn + 16 * j + 4 * q + i, c = n < g.N ? n : g.N - 1;
+        sb[j][i] = g.sb[c];
+        bi[j][i] = g.bias ? g.bias[c] : 0.f;
+      }
     __syncthreads();   // the tile before this one has been read
     put(0);
     __syncthreads();
@@ -87,10 +96,31 @@ __global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, i
       if (more) put(half ^ 1);   // (read last in the stage before, behind a meeting)
       __syncthreads();
     }
+    // outputs: each wave turns 16 tokens at a time through its own part of the
+    // LDS, so that neighbouring lanes store what lies together
+    constexpr int EB = DT == ARCHEAD_F32 ? 4 : 2, OROW = T / 2 * EB + 16, LPR = T / 2 * EB / 16;   // lanes to a token
+    static_assert(4 * 16 * OROW <= int(sizeof(la)), "the waves' parts fit");
+    uint8_t* const buf = reinterpret_cast<uint8_t*>(&la[0][0]) + wid * 16 * OROW;
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < F; ++i) {
+      const int64_t m16 = m0 + wm + 16 * i;
+      const float sa = g.sa[m16 + lr < g.M ? m16 + lr : g.M - 1];
 #pragma unroll
-      for (int j = 0; j < F; ++j) finish4<DT>(g, m0 + wm + 16 * i + lr, n0 + wn + 16 * j + 4 * q, acc[i][j]);
+      for (int j = 0; j < F; ++j) {
+        float y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = scaled(acc[i][j][c], sa, sb[j][c], bi[j][c]);
+        put4<DT>(buf + lr * OROW + (16 * j + 4 * q) * EB, y);
+      }
+      wave_lds_order();
+#pragma unroll
+      for (int r = lane / LPR; r < 16; r += 64 / LPR) {
+        const int64_t m = m16 + r, n = n0 + wn + lane % LPR * (16 / EB);
+        const uint4 v = *reinterpret_cast<const uint4*>(buf + r * OROW + lane % LPR * 16);
+        if (m < g.M) store_part<EB>(g.out + (m * g.ldo + n) * EB, v, g.N - n);
+      }
+      wave_lds_order();
+    }
   }
 }
 
@@ -114,21 +144,54 @@ int compute_units() {
   return n;
 }
 
+// A round of k_i8_split's tiles takes about as long to begin and end as this many
+// k: us of it / tiles of 64 for 64 x 16384 x 256 9.1 / 7.1, 64 x 20000 x 128
+// 10.8 / 7.1 (4 and 5 rounds).
+constexpr int64_t kSplitStart = 1024;
+
+// Rows of a and b that a CU loads with tiles of tm x tn: a round of tiles is
+// bound by them, but for the tallest.
+int64_t rows_loaded(const I8Args& g, int tm, int tn, int n_cu) {
+  const int64_t tiles = (g.M + tm - 1) / tm * ((g.N + tn - 1) / tn);
+  return (tiles + n_cu - 1) / n_cu * (tm + tn);
+}
+
 template <int DT>
 hipError_t launch_matmul(const I8Args& g, hipStream_t s) {
   if (pieces(g)) {
     const int n_cu = compute_units();
-    // From 9 tokens on the tiles' stores of 64 bytes and more of a token tell,
-    // where there is a tile for every CU: us of the two M = 8 / 16 at N = 262144,
-    // K = 2560 121 / 127 and 120 / 122; M = 8 at N = 16384, K = 4096 14 and 23.
-    const bool few = few_take(g) && (g.M <= 8 || (g.N + 255) / 256 < n_cu || !tiles_take(g));
-    if (few) return launch_few<DT>(g, n_cu, s);
-    if (tiles_take(g)) return launch_tiles<DT>(g, n_cu, s);
+    // Up to 16 tokens and above 4 units of channels to a CU, waves that stream
+    // units rather than parts of them: us of split / few at K = 4096 for 1 x 8192
+    // 7.5 / 9.3, 16 x 16384 13.5 / 16.1, 8 x 28672 24.1 / 23.1.  From 9 tokens on
+    // the tiles' stores of 64 bytes and more of a token tell, where there is a
+    // tile for every CU: us of few / tiles for M = 8 / 16 at N = 262144, K = 2560
+    // 121 / 127 and 120 / 122.
+    if (few_take(g) && (g.N + 15) / 16 > 4 * n_cu && (g.M <= 8 || (g.N + 255) / 256 < n_cu || !tiles_take(g)))
+      return launch_few<DT>(g, n_cu, s);
+    // Else the way that loads the fewest bytes a CU: us of split / tiles of 64 for
+    // 64 x 8192 x 4096 10 / 19 (128 / 320 rows), 121 x 1325 x 8704 9 / 35 (64 / 320),
+    // 256 x 4096 x 4096 18 / 19 (256 / 320), 64 x 28672 x 4096 48 / 32 (448 / 320);
+    // of tiles of 64 / 128 / 192 / 256 for 64 x 151936 x 4096 127 / 140 / - / 167,
+    // 333 x 50257 x 1536 63 / 53 / 48 / 51, 512 x 128256 x 8192 795 / 548 / 576 / 485.
+    const int f = g.M <= 16 ? 1 : 2;
+    int64_t best = split_take(g) ? rows_loaded(g, 16 * f, 16 * f, n_cu) * (g.K + kSplitStart) : INT64_MAX;
+    int tm = 0;
+    if (tiles_take(g))
+      for (int t : {256, 192, 128, 64}) {
+        const int64_t bytes = rows_loaded(g, t, 256, n_cu) * g.K;
+        if (bytes < best) {
+          best = bytes;
+          tm = t;
+        }
+      }
+    if (tm) return launch_tiles<DT>(g, tm, n_cu, s);
+    if (best < INT64_MAX) return launch_split<DT>(g, f, s);
   }
-  // us with 128 / 64: 1172 x 43472 x 4229 451 / 727, 200 x 30000 x 1001 25 / 36,
-  // 4096 x 4096 x 4095 116 / 203, but 3127 x 3460 x 141 25 / 21.
+  // us with 128 / 64: 1172 x 43472 x 4229 440 / 721, 200 x 30000 x 1001 21 / 34,
+  // 4096 x 4096 x 4095 113 / 197, 1696 x 67301 x 203 147 / 194, 3127 x 3460 x 141
+  // 17 / 17, but 1000 x 20000 x 100 22 / 21.
   const int64_t large = ((g.M + 127) / 128) * ((g.N + 127) / 128);
-  return large >= 400 && g.K > 2 * kAK ? launch_any<DT, 128>(g, s) : launch_any<DT, 64>(g, s);
+  return large >= 400 && g.K > kAK ? launch_any<DT, 128>(g, s) : launch_any<DT, 64>(g, s);
 }
 
 }  // namespace

@@ -126,7 +126,7 @@ hipError_t launch_rows(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes
                  hipStream_t s) {
   const int64_t groups = SHORT ? (M + 15) / 16 : M, waves = SHORT ? 4 : (d + 512 * HELD - 1) / (512 * HELD);
   const int64_t most = kQMost / 64;
-  return launch_kernel(k_quantize<DT, SHORT, HELD>, dim3(unsigned(groups < (1 << 22) ? groups : 1 << 22)),
+  return launch_kernel(k_quantize<DT, SHORT, HELD>, dim3(unsigned(groups < (1 << 21) ? groups : 1 << 21)),
                        dim3(unsigned(64 * (waves < most ? waves : most))), 0, s, x, M, d, row_bytes, codes, ldc, scales);
 }
 template <int DT>

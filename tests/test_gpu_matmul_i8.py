@@ -215,6 +215,71 @@ def test_matmul_few_tokens(M, N, K, dtype):
     _run_product(M, N, K, dtype, M % 2 == 1, seed=N)
 
 
+# The same with so many channels that b is streamed in units, where a fills half
+# of the LDS and more
+@pytest.mark.parametrize("M,N,K", [(8, 17003, 8192), (16, 20003, 4096), (2, 16500, 16384), (1, 16401, 272)])
+def test_matmul_few_tokens_long_rows(M, N, K):
+    _run_product(M, N, K, "bf16", True, seed=K)
+
+
+# K split over the waves of a workgroup: shares of no stage up to many, K that
+# ends inside a stage, in tiles of 16 and of 32 rows, and tiles of the last XCD only
+@pytest.mark.parametrize("K", [16, 112, 128, 144, 896, 1024, 1040, 2064, 14336])
+@pytest.mark.parametrize("M,N", [(1, 130), (16, 1000), (5, 4099), (17, 1003), (33, 31), (97, 1325), (256, 515)])
+def test_matmul_split_depths(M, N, K):
+    _run_product(M, N, K, "bf16", True, seed=M + K)
+
+
+# Rows at any byte in large tiles: one stage, two, many
+@pytest.mark.parametrize("M,N,K", [(2100, 3001, 333), (700, 9003, 129), (1500, 5001, 1001), (513, 12345, 255)])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_matmul_any_alignment_of_many_tiles(M, N, K, dtype):
+    _run_product(M, N, K, dtype, True, seed=M)
+
+
+# Strided operands and outputs inside a wider buffer, streamed in units, in tiles
+# of every height and at any byte
+@pytest.mark.parametrize("M,N,K,lda,ldb", [(3, 40003, 144, 160, 192), (40, 40003, 144, 160, 192),
+                                           (120, 66001, 128, 144, 160), (180, 67003, 64, 80, 112),
+                                           (250, 66001, 128, 176, 128), (700, 9003, 130, 133, 141)])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_matmul_strided_rows_of_many_channels(M, N, K, lda, ldb, dtype):
+    from paper_2608_02703_amd import matmul_i8
+    host, (a, sa, b, sb, bi) = _operands(M, N, K, M, True, lda=lda, ldb=ldb, off=16)
+    ldo, off = N + 5, 3
+    flat = torch.full((off + M * ldo + 64,), -7.0, dtype=DTYPES[dtype], device="cuda")
+    out = flat[off:].as_strided((M, N), (ldo, 1))
+    matmul_i8(a, sa, b, sb, bias=bi, out=out)
+    _check_product(host, out, dtype)
+    mask = torch.ones_like(flat, dtype=torch.bool)
+    mask[off:].as_strided((M, N), (ldo, 1)).fill_(False)
+    assert (flat[mask] == -7.0).all()
+
+
+# As in use: captured with the quantisation, where b is streamed in units and where
+# workgroups take several tiles
+@pytest.mark.parametrize("M,N", [(4, 30000), (16, 30000), (64, 70000), (200, 70000)])
+def test_matmul_of_many_channels_in_a_graph(M, N):
+    from paper_2608_02703_amd import matmul_i8, quantize_i8
+    K = 256
+    wq, ws = quantize_i8(torch.randn((N, K), device="cuda").to(torch.bfloat16))
+    x = torch.randn((M, K), device="cuda").to(torch.bfloat16)
+    run = lambda: matmul_i8(*quantize_i8(x), wq, ws)   # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for _ in range(3):
+        x.copy_(torch.randn((M, K), device="cuda").to(torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, run())
+
+
 @pytest.mark.parametrize("M,N", [(1, 33), (20, 33), (70, 260), (300, 260)])
 def test_matmul_largest_sums(M, N):
     """K at its limit with all codes -128: 131071 * 2^14 < 2^31."""
