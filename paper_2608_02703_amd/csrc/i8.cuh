@@ -81,6 +81,26 @@ __device__ __forceinline__ void finish4(const I8Args& g, int64_t m, int64_t n, c
   else store_part<EB>(g.out + (m * g.ldo + n) * EB, uint2{w[0], w[1]}, g.N - n);
 }
 
+// bytes k .. k + 15 of a row of K (k < K) at any address, zeros past K
+__device__ __forceinline__ uint4 row_piece(const int8_t* row, int k, int K) {
+  if (__builtin_expect(K < 16, 0)) {
+    uint32_t d[4] = {};
+    for (int j = 0; j < K; ++j) d[j / 4] |= uint32_t(uint8_t(row[j])) << (8 * (j % 4));
+    return uint4{d[0], d[1], d[2], d[3]};
+  }
+  // the row's last 16 bytes, moved down, where fewer are left
+  const int over = max(k + 16 - K, 0);
+  uint4 w = load_any<uint4>(row + k - over);
+  if (over) {
+    uint64_t lo = uint64_t(w.y) << 32 | w.x, hi = uint64_t(w.w) << 32 | w.z;
+    const int bits = 8 * over;
+    lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+    hi = bits < 64 ? hi >> bits : 0;
+    w = uint4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
+  }
+  return w;
+}
+
 // LDS accesses of one wave stay in this order (the hardware keeps it; lanes
 // read what other lanes wrote, which the compiler does not see).
 __device__ __forceinline__ void wave_lds_order() {
@@ -90,8 +110,8 @@ __device__ __forceinline__ void wave_lds_order() {
 
 constexpr int64_t kMaxLd = 1 << 22;   // a tile's rows stay within 31-bit offsets
 
-// What the kernels below need: 16-byte pieces that lie whole in a row and in
-// aligned memory.
+// What the kernels below need, but for launch_loose's: 16-byte pieces that lie
+// whole in a row and in aligned memory.
 inline bool pieces(const I8Args& g) {
   return aligned(g.a, 16) && aligned(g.b, 16) && g.K % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0;
 }
@@ -102,6 +122,8 @@ hipError_t launch_few(const I8Args& g, int n_cu, hipStream_t s);
 bool split_take(const I8Args& g);
 template <int DT>   // in tiles of 16 f x 16 f, f = 1 or 2
 hipError_t launch_split(const I8Args& g, int f, hipStream_t s);
+template <int DT>   // as launch_split, rows at any byte
+hipError_t launch_loose(const I8Args& g, int f, int n_cu, hipStream_t s);
 bool tiles_take(const I8Args& g);
 template <int DT>   // in tiles of tm x 256, tm = 64, 128, 192 or 256
 hipError_t launch_tiles(const I8Args& g, int tm, int n_cu, hipStream_t s);

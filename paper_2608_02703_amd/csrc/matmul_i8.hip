@@ -13,6 +13,8 @@ using namespace archead::i8;
 // waves of T/2 x T/2.  Rows that begin at any byte cannot be loaded to LDS
 // directly: each thread loads its pieces of the next stage into registers while
 // the waves multiply this one, and puts them into the other half of LDS after.
+// Bound by those loads' and their shifts' instructions: 4096 x 4096 x 4095 113 us (1.2
+// POP/s; 4096 x 4096 x 4096 in tiles of aligned rows 63).
 constexpr int kABlock = 256, kAK = 128, kARow = kAK + 16;   // (rows padded: no bank is hit twice as often)
 
 template <int DT, int T>
@@ -24,33 +26,15 @@ __global__ __launch_bounds__(kABlock) void k_i8_any(I8Args g, int64_t m_tiles, i
   for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
     const int64_t m0 = t % m_tiles * T, n0 = t / m_tiles * T;
     uint4 wa[NP], wb[NP];
-    auto piece = [&](const int8_t* base, int64_t r, int64_t rows, int64_t ld, int k) {
-      uint4 w{0, 0, 0, 0};
-      if (r >= rows || k >= g.K) return w;
-      const int8_t* const row = base + r * ld;
-      if (__builtin_expect(g.K < 16, 0)) {
-        uint32_t d[4] = {};
-        for (int j = 0; j < g.K; ++j) d[j / 4] |= uint32_t(uint8_t(row[j])) << (8 * (j % 4));
-        return uint4{d[0], d[1], d[2], d[3]};
-      }
-      // the row's last 16 bytes, moved down, where fewer are left
-      const int over = max(k + 16 - g.K, 0);
-      w = load_any<uint4>(row + k - over);
-      if (over) {
-        uint64_t lo = uint64_t(w.y) << 32 | w.x, hi = uint64_t(w.w) << 32 | w.z;
-        const int bits = 8 * over;
-        lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
-        hi = bits < 64 ? hi >> bits : 0;
-        w = uint4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
-      }
-      return w;
+    auto piece = [&](int64_t r, int64_t rows, const int8_t* base, int64_t ld, int k) {
+      return r < rows && k < g.K ? row_piece(base + r * ld, k, g.K) : uint4{0, 0, 0, 0};
     };
     auto fetch = [&](int k0) {
       const int k = k0 + tid % 8 * 16;
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        wa[i] = piece(g.a, m0 + tid / 8 + 32 * i, g.M, g.lda, k);
-        wb[i] = piece(g.b, n0 + tid / 8 + 32 * i, g.N, g.ldb, k);
+        wa[i] = piece(m0 + tid / 8 + 32 * i, g.M, g.a, g.lda, k);
+        wb[i] = piece(n0 + tid / 8 + 32 * i, g.N, g.b, g.ldb, k);
       }
     };
     auto put = [&](int half) {
@@ -158,8 +142,8 @@ int64_t rows_loaded(const I8Args& g, int tm, int tn, int n_cu) {
 
 template <int DT>
 hipError_t launch_matmul(const I8Args& g, hipStream_t s) {
+  const int n_cu = compute_units();
   if (pieces(g)) {
-    const int n_cu = compute_units();
     // Up to 16 tokens and above 4 units of channels to a CU, waves that stream
     // units rather than parts of them: us of split / few at K = 4096 for 1 x 8192
     // 7.5 / 9.3, 16 x 16384 13.5 / 16.1, 8 x 28672 24.1 / 23.1.  From 9 tokens on
@@ -187,11 +171,16 @@ hipError_t launch_matmul(const I8Args& g, hipStream_t s) {
     if (tm) return launch_tiles<DT>(g, tm, n_cu, s);
     if (best < INT64_MAX) return launch_split<DT>(g, f, s);
   }
+  // K split over waves where there is not a tile for every CU: us of split / tiles
+  // of 64 for 1 x 4096 x 4095 7.3 / 24, 120 x 1500 x 5001 12 / 36, 64 x 8192 x 2001
+  // 11 / 17, 256 x 4096 x 4095 (256 tiles) 28 / 31, but 1 x 50000 x 1001 16 / 13,
+  // 100 x 30000 x 1001 29 / 19.
+  const auto tiles = [&](int t) { return (g.M + t - 1) / t * ((g.N + t - 1) / t); };
+  if (g.K > 0 && tiles(64) <= n_cu) return launch_loose<DT>(g, g.M <= 16 ? 1 : 2, n_cu, s);
   // us with 128 / 64: 1172 x 43472 x 4229 440 / 721, 200 x 30000 x 1001 21 / 34,
   // 4096 x 4096 x 4095 113 / 197, 1696 x 67301 x 203 147 / 194, 3127 x 3460 x 141
   // 17 / 17, but 1000 x 20000 x 100 22 / 21.
-  const int64_t large = ((g.M + 127) / 128) * ((g.N + 127) / 128);
-  return large >= 400 && g.K > kAK ? launch_any<DT, 128>(g, s) : launch_any<DT, 64>(g, s);
+  return tiles(128) >= 400 && g.K > kAK ? launch_any<DT, 128>(g, s) : launch_any<DT, 64>(g, s);
 }
 
 }  // namespace

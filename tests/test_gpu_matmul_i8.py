@@ -230,6 +230,14 @@ def test_matmul_split_depths(M, N, K):
     _run_product(M, N, K, "bf16", True, seed=M + K)
 
 
+# The same with rows at any byte, and with too few stages for every wave
+@pytest.mark.parametrize("K", [1, 15, 17, 127, 255, 257, 513, 1023, 2049, 5003])
+@pytest.mark.parametrize("M,N", [(1, 130), (16, 1000), (5, 4099), (3, 16001), (17, 1003), (33, 31), (97, 1325), (256, 515),
+                                 (60, 8190)])
+def test_matmul_split_depths_at_any_alignment(M, N, K):
+    _run_product(M, N, K, "f16", True, seed=M + K)
+
+
 # Rows at any byte in large tiles: one stage, two, many
 @pytest.mark.parametrize("M,N,K", [(2100, 3001, 333), (700, 9003, 129), (1500, 5001, 1001), (513, 12345, 255)])
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
