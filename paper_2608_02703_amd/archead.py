@@ -426,7 +426,8 @@ def _beam_call(gpu, device, scores, n, finished, end_token, ws, ws_bytes, call):
     if not 1 <= n <= TOPK_MAX:
         raise ValueError(f"n must be in 1 .. {TOPK_MAX}")
     out = torch.empty((B, n), dtype=torch.float32, device=device)
-    parents, tokens = torch.empty((2, B, n), dtype=torch.int64, device=device).unbind(0)
+    parents = torch.empty((B, n), dtype=torch.int64, device=device)
+    tokens = torch.empty((B, n), dtype=torch.int64, device=device)
     ended = torch.empty((B, n), dtype=torch.bool, device=device) if end_token >= 0 else None
     if ws is None:
         ws = torch.empty(max(ws_bytes(B * K), 256), dtype=torch.uint8, device=device)

@@ -100,16 +100,17 @@ __device__ __forceinline__ bool row_counts(const ScanArgs& a, int64_t r) {
   return fabsf(a.scores[r]) < INFINITY && !(a.finished && a.finished[r]);
 }
 
-// Span sp of row r, by a wave: its chunks' largest logits to cmax, its sum of
-// exponentials to *span.
-template <int DT, bool FINE>
-__device__ __forceinline__ void scan_span(const ScanArgs& a, int64_t r, int64_t sp, int lane, float* cmax,
-                                          archead::BeamSpanSum* span) {
+// Span sp of row r, by a wave: its logits, then its chunks' largest to cmax and its
+// sum of exponentials to *span.
+template <int DT>
+__device__ __forceinline__ void load_span(Eight<DT> (&e)[kSteps], const ScanArgs& a, int64_t r, int64_t sp, int lane) {
   const uint8_t* row = a.logits + r * a.row_bytes;
-  Eight<DT> e[kSteps];
 #pragma unroll
   for (int c = 0; c < kSteps; ++c)
     e[c].load(row, sp * archead::kBeamSpan + c * 512 + lane * 8, a.V, neg_inf<DT>());
+}
+template <int DT, bool FINE>
+__device__ __forceinline__ void scan_span(const Eight<DT> (&e)[kSteps], int lane, float* cmax, archead::BeamSpanSum* span) {
   float cm[kSteps], top = -INFINITY;   // cm: of 16 lanes
 #pragma unroll
   for (int c = 0; c < kSteps; ++c) {
@@ -146,7 +147,9 @@ __global__ __launch_bounds__(kScanBlock) void k_beam_scan(ScanArgs a) {
   const int64_t r = blockIdx.y, sp = int64_t(blockIdx.x) * (kScanBlock / 64) + wid;
   if (sp >= a.n_span || !row_counts(a, r)) return;
   const int64_t i = r * a.n_span + sp;
-  scan_span<DT, FINE>(a, r, sp, lane, a.cmax + i * span_chunks(FINE), a.span + i);
+  Eight<DT> e[kSteps];
+  load_span<DT>(e, a, r, sp, lane);
+  scan_span<DT, FINE>(e, lane, a.cmax + i * span_chunks(FINE), a.span + i);
 }
 
 constexpr int kPickBlock = 1024, kPickWaves = kPickBlock / 64;
@@ -156,6 +159,7 @@ constexpr int kPickSpans = 4;    // spans whose sums a lane keeps
 constexpr int kPickGroups = kPickBlock / 16;   // groups of threads that share a maximum
 constexpr int kPickList = 512;   // chunks, and pairs, that are ranked one against all
 static_assert(kPickList >= archead::kTopKMaxK + ARCHEAD_BEAM_MAX, "room for the n best and the ended beams");
+constexpr int kFewSpans = 2 * kPickWaves;   // spans of a sequence up to which there is no first launch
 constexpr int kFineMost = 64;    // spans of a sequence up to which the chunks are the smaller ones
 constexpr int kPickRank = 96;    // pairs up to which no second floor is looked for
 static_assert(kPickGroups == 64, "a lane of a wave for each");
@@ -178,12 +182,11 @@ __device__ __forceinline__ bool before(double sa, uint64_t ia, double sb, uint64
   return sa > sb || (sa == sb && ia < ib);
 }
 
-// FEW: no more spans in a sequence than waves, which read them here (no first
-// launch)
+// FEW: few spans in a sequence, which the waves read here (no first launch)
 template <int DT, bool FINE, bool FEW>
 __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
-  __shared__ float few_cmax[FEW ? kPickWaves * span_chunks(FINE) : 1];
-  __shared__ archead::BeamSpanSum few_span[FEW ? kPickWaves : 1];
+  __shared__ float few_cmax[FEW ? kFewSpans * span_chunks(FINE) : 1];
+  __shared__ archead::BeamSpanSum few_span[FEW ? kFewSpans : 1];
   __shared__ double lse[ARCHEAD_BEAM_MAX], cum[ARCHEAD_BEAM_MAX];   // lse: NaN where a row offers nothing by its logits
   __shared__ bool ended[ARCHEAD_BEAM_MAX];
   __shared__ uint32_t skey[kPickGroups], lane_key[kPickBlock];
@@ -200,9 +203,18 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   const int n_chunk = int((a.V + chunk_logits(FINE) - 1) / chunk_logits(FINE)), n_items = n_chunk * p.K;   // (K V / 512 < 2^27)
   if (tid == 0) n_list = n_pair = 0;
   if constexpr (FEW) {
-    const int k = wid / n_span;
-    if (k < p.K && row_counts(a, r0 + k))
-      scan_span<DT, FINE>(a, r0 + k, wid - k * n_span, lane, few_cmax + wid * span_chunks(FINE), few_span + wid);
+    // the loads of a wave's two spans together
+    Eight<DT> e[2][kSteps];
+    bool use[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = wid + u * kPickWaves, k = i / n_span;
+      use[u] = k < p.K && row_counts(a, r0 + k);
+      if (use[u]) load_span<DT>(e[u], a, r0 + k, i - k * n_span, lane);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (use[u]) scan_span<DT, FINE>(e[u], lane, few_cmax + (wid + u * kPickWaves) * span_chunks(FINE), few_span + wid + u * kPickWaves);
     __syncthreads();
   }
   auto cmax_of = [&](int item) {
@@ -530,9 +542,10 @@ hipError_t launch_select_as(const PickArgs& p, int64_t B, hipStream_t s) {
 
 template <int DT>
 hipError_t launch_select(const PickArgs& p, int64_t B, hipStream_t s) {
-  // One launch where every wave has at most one span of a sequence (GPU time is
-  // the same, a launch takes the host 3 us).
-  if (p.in.n_span * p.K <= kPickWaves)
+  // One launch where a wave has two spans of a sequence at most: us with two
+  // launches / one in a loop of calls 15.7 / 12.6 (a launch takes the host 3), replayed
+  // from a graph 9.3 / 9.3 at 20 spans and 9.9 / 11.3 at 30; at 64 in one 8.8 / 16.
+  if (p.in.n_span * p.K <= kFewSpans)
     return launch_kernel(k_beam_pick<DT, true, true>, dim3(unsigned(B)), dim3(kPickBlock), 0, s, p);
   // us with chunks of 128 / 512: 12 x 16 beams over 4320 tokens 11.6 / 25, 4 over
   // 32000 (64 spans) 8.6 / 9.3, over 50257 (100) 9.2 / 8.6, 8 x 4 over 151936 15.3 / 13.1.
@@ -655,10 +668,10 @@ archead_status archead_beam_select(const void* logits, archead_dtype logits_dtyp
   archead_status st = archead::beam_check(B, K, V, scores, finished, end_token, n, out_scores, parents, tokens);
   if (st != ARCHEAD_OK || B == 0) return st;
   if (ldl < V) return fail(ARCHEAD_E_INVALID_ARG, "ldl < V");
+  const archead::BeamLayout w = archead::beam_layout(B * K, V);
   if (!logits || !ws) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
   if (!aligned(logits, dtype_bytes(logits_dtype)) || !aligned(ws, 256))
     return fail(ARCHEAD_E_MISALIGNED, "logits / workspace misaligned");
-  const archead::BeamLayout w = archead::beam_layout(B * K, V);
   if (ws_bytes < w.total) return fail(ARCHEAD_E_WORKSPACE, "workspace of %zu bytes, %zu needed", ws_bytes, w.total);
   char* base = static_cast<char*>(ws);
   PickArgs p{};

@@ -100,6 +100,22 @@ def test_select(B, K, V, n, dtype):
     check(lg, scores, n, beam_select(lg, scores, n))
 
 
+# Sequences around the spans that one launch reads, with beams that are not read
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("B,K,V,n", [(1, 1, 65536, 4), (1, 1, 65537, 4), (3, 2, 32767, 8), (3, 3, 20480, 6), (2, 4, 16384, 8),
+                                     (2, 4, 16385, 8), (2, 16, 4096, 32), (2, 17, 2048, 17), (5, 32, 2048, 64), (2, 32, 2049, 8),
+                                     (40, 5, 9000, 10)])
+def test_select_of_few_spans(B, K, V, n, dtype):
+    from paper_2608_02703_amd import beam_select
+    lg, scores = _case(B, K, V, dtype, K * V)
+    check(lg, scores, n, beam_select(lg, scores, n))
+    if K > 1:
+        scores[:, K // 2] = -torch.inf
+        fin = torch.zeros((B, K), dtype=torch.bool, device="cuda")
+        fin[:, K - 1] = True
+        check(lg, scores, n, beam_select(lg, scores, n, finished=fin, end_token=V - 1), finished=fin, end_token=V - 1)
+
+
 @pytest.mark.parametrize("dtype", sorted(DTYPES))
 @pytest.mark.parametrize("pad", [1, 2, 3, 5, 8])
 def test_select_row_strides(dtype, pad):
