@@ -224,6 +224,31 @@ def test_select_large_offsets_and_far_scores():
     check(lg, scores * 1000, 8, beam_select(lg, scores * 1000, 8))
 
 
+@pytest.mark.parametrize("V", [3000, 40000])
+def test_select_far_rows(V):
+    """Rows of logits at offsets that pass 32 bits."""
+    from paper_2608_02703_amd import beam_select
+    lg, scores = _case(2, 3, V, "f32", V)
+    ld = 450000000
+    far = torch.empty(5 * ld + V, dtype=torch.float32, device="cuda").as_strided((6, V), (ld, 1))
+    far.copy_(lg)
+    check(far, scores, 6, beam_select(far, scores, 6))
+
+
+def test_two_selections_at_once():
+    from paper_2608_02703_amd import beam_select
+    cases = [_case(2, 4, V, "f32", V) for V in (5000, 60000)]
+    want = [beam_select(lg, scores, 8) for lg, scores in cases]
+    torch.cuda.synchronize()
+    got = []
+    for lg, scores in cases * 4:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got.append(beam_select(lg, scores, 8))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(x, y) for x, y in zip(g, want[i % 2]))
+
+
 def test_select_is_reproducible_and_needs_no_clean_workspace():
     from paper_2608_02703_amd import beam_select, lib
     lg, scores = _case(4, 8, 30000, "bf16", 6, sigma=1.0)

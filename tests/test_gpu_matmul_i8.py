@@ -288,6 +288,57 @@ def test_matmul_of_many_channels_in_a_graph(M, N):
         assert torch.equal(out, run())
 
 
+# Rows of b, of a or of the output at offsets that pass 32 bits, in every way that
+# the product is made
+@pytest.mark.parametrize("M,N,K,lda,ldb,ldo", [
+    (3, 2100, 128, 128, 1 << 21, 2100), (40, 2100, 128, 128, 1 << 21, 60000000), (3, 17000, 128, 128, 1 << 18, 1100000000),
+    (40, 70000, 128, 128, 65536, 60000000), (600, 2100, 128, 1 << 22, 128, 2100), (40, 2100, 100, 100, (1 << 21) + 1, 2100),
+    (40, 70001, 100, 60000001, 65537, 60000000), (2000, 4000, 130, 2200001, 131, 4001)])
+def test_matmul_far_rows(M, N, K, lda, ldb, ldo):
+    from paper_2608_02703_amd import matmul_i8
+    rng = np.random.default_rng(M + N)
+    host, dev = [], []
+    for rows, ld in ((M, lda), (N, ldb)):
+        codes = rng.integers(-128, 128, (rows, K)).astype(np.int8)
+        scale = (rng.random(rows) * 0.01).astype(np.float32)
+        view = torch.empty((rows - 1) * ld + K, dtype=torch.int8, device="cuda").as_strided((rows, K), (ld, 1))
+        view.copy_(torch.from_numpy(codes))
+        host += [codes, scale]
+        dev += [view, torch.from_numpy(scale).cuda()]
+    out = torch.empty((M - 1) * ldo + N, dtype=torch.bfloat16, device="cuda").as_strided((M, N), (ldo, 1))
+    matmul_i8(*dev, out=out)
+    _check_product((*host, None), out, "bf16")
+
+
+def test_quantize_far_rows():
+    from paper_2608_02703_amd import quantize_i8
+    for d in (300, 5001):
+        ld = 1200000000
+        x = torch.empty(2 * ld + d, dtype=torch.float16, device="cuda").as_strided((3, d), (ld, 1))
+        x.copy_(torch.randn((3, d)))
+        codes = torch.empty(2 * ld + d, dtype=torch.int8, device="cuda").as_strided((3, d), (ld, 1))
+        scales = quantize_i8(x, codes=codes)[1]
+        _check_codes(x, codes, scales)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 20000, 1024), (40, 3000, 4096), (200, 70000, 512), (40, 3000, 4095), (300, 20000, 500)])
+def test_two_products_at_once(M, N, K):
+    """On two streams, of the same operands and of one operand with itself."""
+    from paper_2608_02703_amd import matmul_i8
+    _, (a, sa, b, sb, bi) = _operands(M, N, K, 5, True)
+    want, own = matmul_i8(a, sa, b, sb, bias=bi), matmul_i8(a, sa, a, sa)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append((matmul_i8(a, sa, b, sb, bias=bi), matmul_i8(a, sa, a, sa)))
+    torch.cuda.synchronize()
+    for x, y in got:
+        assert torch.equal(x, want) and torch.equal(y, own)
+
+
 @pytest.mark.parametrize("M,N", [(1, 33), (20, 33), (70, 260), (300, 260)])
 def test_matmul_largest_sums(M, N):
     """K at its limit with all codes -128: 131071 * 2^14 < 2^31."""
