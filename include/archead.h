@@ -194,7 +194,12 @@ void archead_destroy(archead_handle* h);
  * V * (r_c + r_r + 4 * (d/g + 3)) bytes, used only while the head has no
  * prepared buffer, see archead_prepare), and for the CE call the
  * per-vocabulary-tile softmax partials.  Returns 0 for a NULL handle or
- * M < 0. */
+ * M < 0.
+ * The compute calls of a handle may be captured into HIP graphs (without
+ * timing events); a replay serves the inputs as they are then.  On the decode,
+ * several-token and GEMV kernels a captured call has one small launch more,
+ * which clears the stamps of the replay before.  Replays whose calls share a
+ * workspace must not run at the same time. */
 size_t archead_workspace_bytes(const archead_handle* h, int64_t M, archead_op op);
 
 /* logits[m, v] for m < M, v < V.

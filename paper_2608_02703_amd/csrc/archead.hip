@@ -597,6 +597,30 @@ uint32_t next_epoch() {
   return counter.fetch_add(1, std::memory_order_relaxed) + 1u;
 }
 
+// A call captured into a HIP graph has the same stamp in every replay, so the
+// words that the replay before left would pass for this one's.  There the head
+// stream's launches follow one that gives all words another stamp.
+__global__ __launch_bounds__(kBlock) void k_unstamp(unsigned long long* tst, int64_t n, uint32_t epoch) {
+  for (int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x; i < n; i += int64_t(gridDim.x) * kBlock)
+    __hip_atomic_store(tst + i, static_cast<unsigned long long>(~epoch) << 32, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+archead_status unstamp_captured(const Stage1Ops& o, int64_t M, hipStream_t s) {
+  unsigned long long* tst = o.tst;
+  int64_t n = M * (o.rc + o.rr);
+  if (!s || n == 0) return ARCHEAD_OK;   // (the default stream is never captured)
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(s, &st);
+  if (e != hipSuccess) return hip_fail(e, "stream capture status");
+  if (st == hipStreamCaptureStatusNone) return ARCHEAD_OK;
+  uint32_t epoch = o.epoch;
+  void* args[] = {&tst, &n, &epoch};
+  const int64_t grid = (n + kBlock - 1) / kBlock;
+  e = hipLaunchKernel(reinterpret_cast<const void*>(k_unstamp), dim3(unsigned(grid < 1024 ? grid : 1024)), dim3(kBlock), args,
+                      0, s);
+  return e == hipSuccess ? ARCHEAD_OK : hip_fail(e, "stamp launch");
+}
+
 // Stage-1 operands of a call (V_c, B_w and their scales, the stamped t in
 // the workspace, a fresh epoch).
 Stage1Ops stage1_ops(const archead_handle* h, uint64_t* tst) {
@@ -672,6 +696,8 @@ archead_status launch_gemv_passes(const archead_handle* h, GemvArgs a, int64_t M
                                   int64_t forced_grid, hipStream_t s, bool topk = false,
                                   Part part = {}) {
   const int lpr = lanes_per_row(h->desc);
+  const archead_status st = unstamp_captured(a.s1, M, s);
+  if (st != ARCHEAD_OK) return st;
   const Timing ev = timing_events(h, part);
   for (int64_t m0 = 0; m0 < M; m0 += 4) {
     const int tok = int(M - m0 < 4 ? M - m0 : 4);
@@ -709,6 +735,8 @@ archead_status launch_dec(const archead_handle* h, const void* x, int64_t M, int
   a.ca = static_cast<const int8_t*>(h->ptrs.corr_a);
   a.sa = static_cast<const uint16_t*>(h->ptrs.corr_a_scale);
   a.s1 = stage1_ops(h, tst);
+  const archead_status st = unstamp_captured(a.s1, M, s);
+  if (st != ARCHEAD_OK) return st;
   a.x = static_cast<const uint16_t*>(x);
   a.ldx = ldx;
   a.V = d.V;
@@ -762,6 +790,8 @@ archead_status launch_mid(const archead_handle* h, const void* x, int64_t M, int
   a.ca = static_cast<const int8_t*>(h->ptrs.corr_a);
   a.sa = static_cast<const uint16_t*>(h->ptrs.corr_a_scale);
   a.s1 = stage1_ops(h, tst);
+  const archead_status st = unstamp_captured(a.s1, M, s);
+  if (st != ARCHEAD_OK) return st;
   a.x = static_cast<const uint16_t*>(x);
   a.ldx = ldx;
   a.V = d.V;
