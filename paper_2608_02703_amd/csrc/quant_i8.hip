@@ -18,8 +18,8 @@ constexpr int kQShort = 512;     // longest row that 16 lanes take
 // With s the scale, x * (1 / s) + 1.5 * 2^23 (one rounding) ends in the integer
 // q nearest to x / s or next to it, in two's complement.  r = x - q s is exact (a
 // multiple of the smaller of the two operands' units, and at most about s / 2),
-// so comparing it with s / 2 (exact) says which integer is nearest, and which way
-// a half goes.
+// so comparing 2 r with s (s / 2 is no fp32 number where s is an odd multiple of
+// 2^-149) says which integer is nearest, and which way a half goes.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {   // another lane of the row of 16
   return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false));
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t
     if (!live) continue;
     const bool finite = top < 0x7f800000u;
     const float s = finite ? fmaxf(__uint_as_float(top) / 127.f, 0x1p-126f) : NAN;
-    const float inv = finite ? 1.f / s : 0.f, half = 0.5f * s;
+    const float inv = finite ? 1.f / s : 0.f;
     if (t == 0) scales[m] = s;
     int8_t* out = codes + m * ldc;
     constexpr float kBig = 0x1.8p23f;
@@ -87,12 +87,13 @@ __global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t
         r[i] = fmaf(kBig - t[i], s, v);
         far = fmaxf(far, fabsf(r[i]));
       }
-      if (__builtin_expect(far >= half, 0)) {
+      if (__builtin_expect(far + far >= s, 0)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const bool odd = __float_as_uint(t[i]) & 1;
-          if (r[i] > half || (r[i] == half && odd)) t[i] += 1.f;
-          else if (r[i] < -half || (r[i] == -half && odd)) t[i] -= 1.f;
+          const float twice = r[i] + r[i];
+          if (twice > s || (twice == s && odd)) t[i] += 1.f;
+          else if (twice < -s || (twice == -s && odd)) t[i] -= 1.f;
         }
       }
       uint32_t w[2];
