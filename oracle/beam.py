@@ -23,8 +23,8 @@ def scores_of(logits: np.ndarray, scores: np.ndarray, finished=None, end_token=-
             m = row.max()
             if not np.isfinite(m) or np.isnan(row).any():   # nothing allowed, a NaN, or +inf
                 continue
-            lse = m + np.log(np.exp(row - m).sum())
-            out[b, k] = c + (row - lse)
+            d = row - m   # (m and the log apart: their sum would lose the log beside a large m)
+            out[b, k] = c + (d - np.log(np.exp(d).sum()))
     return out
 
 

@@ -15,7 +15,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Two launches.  k_beam_scan reads the logits once: of every chunk of a row
 // its largest logit, and of every span of chunks (a wave's) the pair (maximum,
 // sum of exponentials).  k_beam_pick, a workgroup per sequence, makes the rows'
-// logsumexp of them and with it the chunks' largest scores.  If n chunks are
+// (maximum, sum) of them and with it the chunks' largest scores.  A score is
+// (score of the beam - log sum) + (logit - maximum): the maximum and the log are
+// not added up, since a row of the type's lowest value would lose the log.  If n chunks are
 // ranked by (largest score, then position), every pair among the n best lies in
 // one of the first n, so the logits of few more than those are read again.
 // The scan is bound by the logits' bytes (256 rows x 262143 bf16: 134 MB in 26 us,
@@ -187,7 +189,9 @@ template <int DT, bool FINE, bool FEW>
 __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
   __shared__ float few_cmax[FEW ? kFewSpans * span_chunks(FINE) : 1];
   __shared__ archead::BeamSpanSum few_span[FEW ? kFewSpans : 1];
-  __shared__ double lse[ARCHEAD_BEAM_MAX], cum[ARCHEAD_BEAM_MAX];   // lse: NaN where a row offers nothing by its logits
+  // of a beam: score, score less the log of its sum (NaN where the row offers
+  // nothing by its logits), largest logit
+  __shared__ double cum[ARCHEAD_BEAM_MAX], base[ARCHEAD_BEAM_MAX], most[ARCHEAD_BEAM_MAX];
   __shared__ bool ended[ARCHEAD_BEAM_MAX];
   __shared__ uint32_t skey[kPickGroups], lane_key[kPickBlock];
   __shared__ Ranked list[kPickList];
@@ -239,10 +243,10 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
       first[u] = lane + 64 * u < n_span ? span_of(k, lane + 64 * u) : archead::BeamSpanSum{0.0, 0.f};
     const float c = a.scores[r0 + k];
     const bool f = a.finished && a.finished[r0 + k];
-    double l = NAN;
+    double from = NAN;
+    float top = -INFINITY;
     if (fabsf(c) < INFINITY && !f) {
       // (a span with nothing above -inf has the sum 0, whatever its maximum)
-      float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kPickSpans; ++u) top = first[u].sum != 0.0 ? fmaxf(top, first[u].top) : top;
       for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) {
@@ -260,19 +264,20 @@ __global__ __launch_bounds__(kPickBlock) void k_beam_pick(PickArgs p) {
       for (int i = lane + 64 * kPickSpans; i < n_span; i += 64) add(span_of(k, i));
       s = wave_sum(s);
       // +inf among the logits: a term inf - inf, so the sum is NaN
-      if (s > 0.0) l = top + log(s);
+      if (s > 0.0) from = c - log(s);
     }
     if (lane == 0) {
-      lse[k] = l;
       cum[k] = c;
+      base[k] = from;
+      most[k] = top;
       ended[k] = f;
     }
   }
   __syncthreads();
-  auto score_of = [&](int k, float logit) { return cum[k] + (double(logit) - lse[k]); };
+  auto score_of = [&](int k, float logit) { return base[k] + (double(logit) - most[k]); };
   auto chunk_score = [&](int item, float top) {
     const int k = item / n_chunk;
-    return lse[k] == lse[k] ? score_of(k, top) : double(-INFINITY);
+    return base[k] == base[k] ? score_of(k, top) : double(-INFINITY);
   };
   auto score_again = [&](int item) { return chunk_score(item, cmax_of(item)); };
   // ---- a floor: about the n-th largest of the groups' best chunks, in the
