@@ -631,9 +631,12 @@ size_t archead_beam_workspace_bytes(int64_t rows, int64_t V);
 /* The n best continuations of each sequence: with
  *   score(k, v) = scores[b, k] + (logit[b K + k, v] - logsumexp(logit[b K + k, :]))
  * for every beam k and token v, the n pairs (k, v) of largest score in
- * decreasing order, equal scores by increasing k, then v.  Within a beam the
- * order is that of the logits; between beams that of scores in fp64 from fp32
- * exponentials summed in a fixed order.  out_scores has the score rounded to
+ * decreasing order, equal scores by increasing k, then v.  A score is the fp64
+ * number (scores[b, k] - log s) + (logit - m), m the row's largest logit and s
+ * the sum of fp32 exponentials of logit - m in a fixed order.  So the order
+ * within a beam is that of the logits, but for those whose difference fp64
+ * loses beside m or the score (1e-18 and 3e-18 beside m = 1): their scores are
+ * equal, and the lower token goes first.  out_scores has the score rounded to
  * fp32.
  *   - Only scores above -inf are candidates: tokens with logit -inf are not,
  *     nor any token of a beam whose own score is not finite (a beam not yet

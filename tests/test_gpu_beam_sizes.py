@@ -1,4 +1,5 @@
-"""beam_select over rows of the type's lowest value, against the formula in 64
+"""beam_select over rows of the type's lowest value and logits whose
+scores coincide, against the formula in 64
 bits and the oracle under the bounds of test_gpu_beam.py."""
 from __future__ import annotations
 
@@ -52,3 +53,16 @@ def test_rows_of_the_lowest_value(V, dtype):
     v = got[0][0].cpu().numpy().astype(np.float64)
     assert (np.abs(v - s[order]) <= bound + 2.0 ** -24 * np.abs(s[order]) * 1.001).all()
     check(lg, scores, n, got)
+
+
+def test_logits_that_differ_by_less_than_a_score_shows():
+    """Scores are fp64: logits of one beam whose scores coincide there go by
+    their tokens."""
+    from paper_2608_02703_amd import beam_select
+    lg = torch.full((2, 9000), -3.0, device="cuda")
+    lg[:, 100], lg[:, 4000], lg[:, 8000] = 1e-18, 3e-18, -1e-18
+    lg[:, 6000] = 1.0
+    scores = torch.tensor([[-1.25, -1.5]], device="cuda")
+    _, parents, tokens = beam_select(lg, scores, 8)
+    assert parents[0].tolist() == [0, 1, 0, 0, 0, 1, 1, 1]
+    assert tokens[0].tolist() == [6000, 6000, 100, 4000, 8000, 100, 4000, 8000]
