@@ -461,6 +461,46 @@ def beam_select(logits, scores, n, finished=None, end_token=-1, ws=None):
                       lambda rows: L.archead_beam_workspace_bytes(rows, V), call)
 
 
+def _extent(t):
+    """[(bytes of a step, steps)] of a tensor, largest step first, and the
+    contiguous bytes that are stepped."""
+    width, steps = t.element_size(), []
+    for st, n in sorted((st * t.element_size(), n) for n, st in zip(t.shape, t.stride()) if n > 1 and st):
+        if not steps and st <= width:
+            width += st * (n - 1)
+        else:
+            steps.insert(0, (st, n))
+    return steps, width
+
+
+def _share_memory(a, b):
+    """Whether two tensors (of a GPU, without negative strides) hold a byte in
+    common: of their steps the largest first, those that bring the rest of both
+    together."""
+    seen = set()
+
+    def reach(steps, width):
+        return sum(st * (n - 1) for st, n in steps) + width
+
+    def meet(sa, sb, off):   # off: the first byte of b's rest from that of a's
+        if off >= reach(sa, wa) or -off >= reach(sb, wb) or (len(sa), len(sb), off) in seen:
+            return False
+        if not sa and not sb:
+            return True
+        seen.add((len(sa), len(sb), off))
+        st = max(sa[:1] + sb[:1])[0]
+        na = nb = 1
+        if sa and sa[0][0] == st:
+            na, sa = sa[0][1], sa[1:]
+        if sb and sb[0][0] == st:
+            nb, sb = sb[0][1], sb[1:]
+        # steps i of b less those of a with  -reach(b's rest) < off + i st < reach(a's rest)
+        lo, hi = -((off + reach(sb, wb) - 1) // st), (reach(sa, wa) - 1 - off) // st
+        return any(meet(sa, sb, off + i * st) for i in range(max(lo, 1 - na), min(hi, nb - 1) + 1))
+    (sa, wa), (sb, wb) = _extent(a), _extent(b)
+    return meet(sa, sb, b.data_ptr() - a.data_ptr())
+
+
 class BeamStates:
     """The states of a beam search's rows (caches of every layer, recurrent
     states, token histories), described once and reordered after every step
@@ -469,9 +509,10 @@ class BeamStates:
     states: tensors on one GPU of beams * B rows along `row_dim`.  out: tensors
     for the reordered states, of out_beams * B rows (default: beams) and
     otherwise alike, sharing no memory with states; or None to reorder the
-    states where they are.  pos_dim: the dimension of the positions, where
-    reorder() is to move the leading ones alone.  Of the remaining dimensions,
-    those that do not lie back to back have to step as one."""
+    states where they are.  No two destinations share memory.  pos_dim: the
+    dimension of the positions, where reorder() is to move the leading ones
+    alone.  Of the remaining dimensions, those that do not lie back to back have
+    to step as one."""
 
     def __init__(self, states, beams, out=None, out_beams=None, row_dim=0, pos_dim=None):
         states = list(states)
@@ -508,9 +549,13 @@ class BeamStates:
             key = self._layout(s, d, r, p)
             if d.numel():
                 groups.setdefault(key, []).append(i)
-        starts = [t.data_ptr() for t in self.out if t.numel()]
-        if len(set(starts)) != len(starts):
-            raise ValueError("two of the destinations are the same memory")
+        open_ = []   # destinations so far that reach the next one's first byte
+        for t in sorted((t for t in self.out if t.numel()), key=lambda t: t.data_ptr()):
+            lo, hi = self._span(t)
+            open_ = [(end, u) for end, u in open_ if end > lo]
+            if any(_share_memory(u, t) for _, u in open_):
+                raise ValueError("two of the destinations share memory")
+            open_.append((hi, t))
         if not self.in_place:
             spans = sorted([(*self._span(t), w) for w, ts in ((0, states), (1, self.out)) for t in ts if t.numel()])
             ends = [-1, -1]
