@@ -549,20 +549,18 @@ class BeamStates:
             key = self._layout(s, d, r, p)
             if d.numel():
                 groups.setdefault(key, []).append(i)
-        open_ = []   # destinations so far that reach the next one's first byte
-        for t in sorted((t for t in self.out if t.numel()), key=lambda t: t.data_ptr()):
+        # by first byte, with those before that reach it: two destinations, or one
+        # and a state, share no memory
+        all_ = [(t, True) for t in self.out] + ([] if self.in_place else [(t, False) for t in states])
+        open_ = []
+        for t, written in sorted(((t, w) for t, w in all_ if t.numel()), key=lambda e: e[0].data_ptr()):
             lo, hi = self._span(t)
-            open_ = [(end, u) for end, u in open_ if end > lo]
-            if any(_share_memory(u, t) for _, u in open_):
-                raise ValueError("two of the destinations share memory")
-            open_.append((hi, t))
-        if not self.in_place:
-            spans = sorted([(*self._span(t), w) for w, ts in ((0, states), (1, self.out)) for t in ts if t.numel()])
-            ends = [-1, -1]
-            for lo, hi, w in spans:
-                if lo < ends[1 - w]:
-                    raise ValueError("out shares memory with states")
-                ends[w] = max(ends[w], hi)
+            open_ = [e for e in open_ if e[0] > lo]
+            for _, u, w in open_:
+                if (written or w) and _share_memory(u, t):
+                    raise ValueError("two of the destinations share memory" if written and w
+                                     else "out shares memory with states")
+            open_.append((hi, t, written))
         self._groups = []
         for key, members in groups.items():
             arr = ctypes.c_void_p * len(members)

@@ -45,3 +45,23 @@ def test_takes_states_that_lie_among_each_other(in_place):
         new = (x, y) if in_place else (u, v)
         for got, old in zip(view(*new), view(a, b)):
             assert torch.equal(got, old[rows])
+
+
+def test_takes_two_buffers_that_lie_among_each_other():
+    """A cache whose rows hold the states before and after a step; sources may
+    be the same memory."""
+    from paper_2608_02703_amd import BeamStates
+    K = 4
+    both = torch.randn((2 * K, 2, 5, 16), generator=torch.Generator().manual_seed(2)).cuda()
+    old = both.clone()
+    q = torch.tensor([[3, 0, 3, 1], [2, 2, 1, 0]], device="cuda")
+    rows = (q + K * torch.arange(2, device="cuda")[:, None]).view(-1)
+    BeamStates([both[:, 0]], K, [both[:, 1]]).reorder(q)
+    assert torch.equal(both[:, 1], old[rows, 0]) and torch.equal(both[:, 0], old[:, 0])
+    out = [torch.zeros((2 * K, 5, 16), device="cuda") for _ in range(2)]
+    for got in BeamStates([both[:, 0]] * 2, K, out).reorder(q):
+        assert torch.equal(got, old[rows, 0])
+    for bad in (lambda: BeamStates([both[:, 0]], K, [both[:, 0]]), lambda: BeamStates([both[:, 0, 1:]], K, [both[:, 0, :4]]),
+                lambda: BeamStates([out[0], both[:, 0]], K, [both[:, 1], out[0]])):
+        with pytest.raises(ValueError, match="out shares memory"):
+            bad()
