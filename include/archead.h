@@ -708,8 +708,9 @@ typedef struct archead_state_layout {
  * Each source row is read once however many beams continue it.  Pointers,
  * strides and pos_bytes that are multiples of 16 are fastest (of 4: less so;
  * of 1: slow).  n_states = 0, B = 0 or empty rows are a no-op.
- * ARCHEAD_E_INVALID_ARG for a null pointer, a negative size or stride, K
- * outside [1, ARCHEAD_BEAM_MAX], n outside [1, ARCHEAD_TOPK_MAX], B >= 2^25, a
+ * ARCHEAD_E_INVALID_ARG for a null pointer, a negative size or stride, a stride
+ * above 2^42, a row of more than 2^45 bytes, states that reach over more than
+ * 2^62, K outside [1, ARCHEAD_BEAM_MAX], n outside [1, ARCHEAD_TOPK_MAX], B >= 2^25, a
  * mixture of states in place and not, in place with n != K or other strides;
  * ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when a launch fails. */
 archead_status archead_beam_reorder(const archead_state_layout* layout, int64_t n_states,

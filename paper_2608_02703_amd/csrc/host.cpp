@@ -187,7 +187,6 @@ archead_status reorder_check(const archead_state_layout* l, int64_t n_states, co
   if (n_states < 0) return fail(ARCHEAD_E_INVALID_ARG, "n_states = %lld", (long long)n_states);
   if (idx_dtype != ARCHEAD_I32 && idx_dtype != ARCHEAD_I64)
     return fail(ARCHEAD_E_INVALID_ARG, "idx_dtype must be I32 or I64");
-  // sizes that keep every product below 2^63
   const int64_t sizes[] = {l->n_outer, l->positions, l->pos_bytes, l->src_row, l->src_outer,
                            l->src_pos, l->dst_row, l->dst_outer, l->dst_pos};
   for (int i = 0; i < 9; ++i)
@@ -195,6 +194,13 @@ archead_status reorder_check(const archead_state_layout* l, int64_t n_states, co
       return fail(ARCHEAD_E_INVALID_ARG, "a size or stride of the layout is out of range (%lld)", (long long)sizes[i]);
   if (double(l->n_outer) * double(l->positions) * double(l->pos_bytes) > 0x1p45)
     return fail(ARCHEAD_E_INVALID_ARG, "a row of more than 2^45 bytes");
+  // the last byte's offset from a state's first, which the kernel forms in 64 bits
+  auto reach = [&](int64_t rows, int64_t row, int64_t outer, int64_t pos) {
+    auto steps = [](int64_t n, int64_t stride) { return n > 1 ? double(n - 1) * double(stride) : 0.0; };
+    return steps(B * rows, row) + steps(l->n_outer, outer) + steps(l->positions, pos) + double(l->pos_bytes);
+  };
+  if (reach(K, l->src_row, l->src_outer, l->src_pos) > 0x1p62 || reach(n, l->dst_row, l->dst_outer, l->dst_pos) > 0x1p62)
+    return fail(ARCHEAD_E_INVALID_ARG, "states of more than 2^62 bytes");
   if (n_states == 0 || B == 0) return ARCHEAD_OK;
   if (!src || !dst || !parents) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
   int64_t same = 0;
