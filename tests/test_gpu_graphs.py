@@ -147,3 +147,11 @@ def test_two_graphs_of_one_workspace(head, path, M):
             torch.cuda.synchronize()
             got = held.clone()
             assert torch.equal(got, head.logits(xs[i]))
+
+
+@pytest.mark.parametrize("M", [1, 70, 300])
+def test_fidelity_to_a_dense_head(head, M):
+    gen = torch.Generator().manual_seed(M)
+    dense = (torch.randn((8192, 512), generator=gen) * 0.05).to(torch.bfloat16).cuda()
+    x = _x(M, 0)
+    _replays(lambda: [*head.logit_fidelity_head(x, dense)], x, _equal)
