@@ -618,6 +618,43 @@ archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const float* a_sc
                                  archead_dtype out_dtype, int64_t ldo, void* stream);
 
 /* ------------------------------------------------------------------------
+ * The root-mean-square norm in front of a head or an INT8 layer, with the
+ * residual's addition and its rows in their own type, rounded to 8 bits, or
+ * both.  For m < M and i < d, with r = 0 where residual is NULL:
+ *   s = x[m, i] + r[m, i],  t = s * (offset + weight[i])   each rounded to fp32
+ *   total[m, i] = s                                  rounded to dtype
+ *   n = sqrt(mean_i s^2 + eps)                       in fp64
+ *   out[m, i]   = t / n                              rounded to dtype
+ *   u = max(max_i |t| / 127 rounded to fp32, 2^-126)
+ *   codes[m, i] = the integer nearest to t / u (the exact quotient; halves to
+ *                 even), in [-127, 127];  scales[m] = u / n rounded to fp32
+ * so codes * scales is out to 8 bits, and feeds archead_matmul_i8.  (out is
+ * formed from t and 1 / n rounded to fp32: off by at most 2^-23 of it before
+ * its rounding.)  A row whose t holds an infinity or a NaN gets out and scale
+ * NaN and codes 0.
+ *   x         fp32, bf16 or fp16 (dtype) [M, ldx] device, 1 <= d <= 16384
+ *   residual  dtype [M, ldr] device or NULL
+ *   weight    dtype or fp32 [d] device;  offset  0, or 1 for weights held as
+ *             w - 1;  eps > 0
+ *   total     dtype [M, ldt] device or NULL;  out  dtype [M, ldo] device or
+ *             NULL;  codes  int8 [M, ldc] device or NULL (any alignment), with
+ *             scales device fp32 [M].  out or codes must be there.
+ *   stream    hipStream_t (NULL = the default stream); asynchronous
+ * Pointers are aligned to their element size, leading dimensions >= d; what
+ * lies between rows is left as it was.  total may be x or residual, and out
+ * may be x, with the same leading dimension (not both x); otherwise outputs share no
+ * memory with inputs or each other.  Results are reproducible.  M = 0 is a
+ * no-op.  ARCHEAD_E_INVALID_ARG for a null pointer, M < 0 or M >= 2^31, d < 1,
+ * a leading dimension < d, an eps that is not positive and finite, an offset
+ * that is not finite, or a dtype not listed; ARCHEAD_E_UNSUPPORTED for
+ * d > 16384; ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when the launch fails. */
+archead_status archead_rms_norm(const void* x, archead_dtype dtype, int64_t M, int64_t d, int64_t ldx,
+                                const void* residual, int64_t ldr, const void* weight,
+                                archead_dtype weight_dtype, float offset, double eps, void* total,
+                                int64_t ldt, void* out, int64_t ldo, int8_t* codes, int64_t ldc,
+                                float* scales, void* stream);
+
+/* ------------------------------------------------------------------------
  * Beam search: the choice of the next hypotheses, and the states they
  * continue.  B sequences of K beams each; row b * K + k belongs to beam k of
  * sequence b.

@@ -19,6 +19,8 @@ from .archead import (  # noqa: F401
     pack_int5,
     packed_bytes,
     quantize_i8,
+    rms_norm,
+    rms_norm_i8,
     unpack_int4,
     unpack_int5,
     validate_desc,

@@ -124,6 +124,11 @@ _SIGS = {
                                          ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
                                          ctypes.c_int64, ctypes.c_void_p, ctypes.c_int,
                                          ctypes.c_int64, ctypes.c_void_p]),
+    "archead_rms_norm": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                        ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                        ctypes.c_int, ctypes.c_float, ctypes.c_double, ctypes.c_void_p,
+                                        ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                        ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
     "archead_beam_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
     "archead_beam_select": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64,
                                            ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
@@ -411,6 +416,62 @@ def matmul_i8(a, a_scales, b, b_scales, bias=None, out=None, out_dtype=None):
     _launch(gpu, lib().archead_matmul_i8, a.data_ptr(), lda, a_scales.data_ptr(), b.data_ptr(), ldb,
             b_scales.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), code, ldo)
     return out
+
+
+def _norm_call(x, weight, eps, residual, offset, total, out, codes, scales):
+    """archead_rms_norm around its checks; returns the sums' tensor, or None."""
+    import torch
+    gpu = _gpu_of(x, "x")
+    ldx = _matrix(x, "x", gpu)
+    code = _float_code(x.dtype, "x")
+    M, d = x.shape
+    _dense(weight, "weight", gpu, (x.dtype, torch.float32), (d,))
+    ldr = ldt = ldo = ldc = d
+    if residual is not None:
+        ldr = _matrix(residual, "residual", gpu, x.dtype, (M, d))
+        if total is None:
+            total = torch.empty((M, d), dtype=x.dtype, device=x.device)
+        else:
+            ldt = _matrix(total, "total", gpu, x.dtype, (M, d))
+    elif total is not None:
+        raise ValueError("total needs a residual")
+    if out is not None:
+        ldo = _matrix(out, "out", gpu, x.dtype, (M, d))
+    if codes is not None:
+        ldc = _matrix(codes, "codes", gpu, torch.int8, (M, d))
+        _dense(scales, "scales", gpu, (torch.float32,), (M,))
+    _launch(gpu, lib().archead_rms_norm, x.data_ptr(), code, M, d, ldx, _ptr(residual), ldr, weight.data_ptr(),
+            _float_code(weight.dtype, "weight"), offset, eps, _ptr(total), ldt, _ptr(out), ldo, _ptr(codes), ldc,
+            _ptr(scales))
+    return total
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None, offset=0.0, out=None, total=None):
+    """Root-mean-square norm of the rows of x (float32, bfloat16 or float16
+    [M, d] on the GPU, d <= 16384), of x + residual where one is given, times
+    offset + weight (archead_rms_norm).  Returns the normed rows, and with a
+    residual (normed rows, x + residual).  total (where the sum goes) may be
+    residual or x, out may be x."""
+    import torch
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    total = _norm_call(x, weight, eps, residual, offset, total, out, None, None)
+    return out if residual is None else (out, total)
+
+
+def rms_norm_i8(x, weight, eps=1e-6, residual=None, offset=0.0, normed=False, codes=None, scales=None, total=None):
+    """rms_norm with its rows rounded to 8 bits, for matmul_i8: returns (codes
+    int8 [M, d], scales float32 [M]), then x + residual where a residual is
+    given, then the rows in x's type where normed is True or a tensor for them
+    (archead_rms_norm)."""
+    import torch
+    if codes is None:
+        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    if scales is None:
+        scales = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if normed is True else None if normed is False else normed
+    total = _norm_call(x, weight, eps, residual, offset, total, out, codes, scales)
+    return (codes, scales) + (() if residual is None else (total,)) + (() if out is None else (out,))
 
 
 def _beam_call(gpu, device, scores, n, finished, end_token, ws, ws_bytes, call):

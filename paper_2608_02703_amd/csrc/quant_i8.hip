@@ -1,5 +1,5 @@
 // archead_quantize_i8: rows to int8 codes and one fp32 scale each.
-#include "dev_rows.cuh"
+#include "dev_codes.cuh"
 
 namespace {
 
@@ -14,17 +14,6 @@ constexpr int kQShort = 512;     // longest row that 16 lanes take
 // largest), and one for the codes; what a thread holds stays in registers in
 // between, longer rows are read again (from the caches).  151936 x 4096 bf16:
 // 312 us (6.0 TB/s); a wave to a row, eight groups a lane: 443.
-//
-// With s the scale, x * (1 / s) + 1.5 * 2^23 (one rounding) ends in the integer
-// q nearest to x / s or next to it, in two's complement.  r = x - q s is exact (a
-// multiple of the smaller of the two operands' units, and at most about s / 2),
-// so comparing 2 r with s (s / 2 is no fp32 number where s is an odd multiple of
-// 2^-149) says which integer is nearest, and which way a half goes.
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp(uint32_t v) {   // another lane of the row of 16
-  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false));
-}
-
 template <int DT, bool SHORT, int HELD>
 __global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t* x, int64_t M, int64_t d, int64_t row_bytes,
                                                       int8_t* codes, int64_t ldc, float* scales) {
@@ -58,10 +47,10 @@ __global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t
       e.load(row, j, n, 0);
       larger(e);
     }
-    top = max(top, dpp<0xB1>(top));
-    top = max(top, dpp<0x4E>(top));
-    top = max(top, dpp<0x141>(top));
-    top = max(top, dpp<0x140>(top));
+    top = max(top, dpp<kDpp1>(top));
+    top = max(top, dpp<kDpp2>(top));
+    top = max(top, dpp<kDpp4>(top));
+    top = max(top, dpp<kDpp8>(top));
     if constexpr (!SHORT) {
       auto of = [&](int l) { return uint32_t(__builtin_amdgcn_readlane(int(top), l)); };
       top = max(max(of(0), of(16)), max(of(32), of(48)));
@@ -77,37 +66,11 @@ __global__ __launch_bounds__(SHORT ? 256 : kQMost) void k_quantize(const uint8_t
     const float inv = finite ? 1.f / s : 0.f;
     if (t == 0) scales[m] = s;
     int8_t* out = codes + m * ldc;
-    constexpr float kBig = 0x1.8p23f;
     auto write = [&](const E& e, int64_t j) {
-      float t[8], r[8], far = 0.f;
+      float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = e.at(i);
-        t[i] = fmaf(v, inv, kBig);
-        r[i] = fmaf(kBig - t[i], s, v);
-        far = fmaxf(far, fabsf(r[i]));
-      }
-      if (__builtin_expect(far + far >= s, 0)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const bool odd = __float_as_uint(t[i]) & 1;
-          const float twice = r[i] + r[i];
-          if (twice > s || (twice == s && odd)) t[i] += 1.f;
-          else if (twice < -s || (twice == -s && odd)) t[i] -= 1.f;
-        }
-      }
-      uint32_t w[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {   // the low bytes of four
-        auto low = [&](int k) { return __float_as_uint(t[4 * i + k]); };
-        const uint32_t a = __builtin_amdgcn_perm(low(1), low(0), 0x0c0c0400), b = __builtin_amdgcn_perm(low(3), low(2), 0x0c0c0400);
-        w[i] = finite ? a | b << 16 : 0u;
-      }
-      if (j + 8 <= d) {
-        store_any(out + j, uint2{w[0], w[1]});
-      } else {
-        for (int i = 0; j + i < d; ++i) out[j + i] = int8_t(w[i / 4] >> (8 * (i % 4)));
-      }
+      for (int i = 0; i < 8; ++i) v[i] = e.at(i);
+      store_codes(out, j, d, codes8(v, s, inv, finite));
     };
 #pragma unroll
     for (int g = 0; g < HELD; ++g) {
