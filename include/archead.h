@@ -655,6 +655,50 @@ archead_status archead_rms_norm(const void* x, archead_dtype dtype, int64_t M, i
                                 float* scales, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Low-rank adapters of many requests at once, beside a projection that they
+ * share (archead_matmul_i8, a head, any other product): for m < M, with i =
+ * ids[m],
+ *   out[m, :] = y[m, :] + scales[i] (x[m, :] a_i^T) b_i^T
+ * and out[m, :] = y[m, :] where i lies outside [0, n): a token without an
+ * adapter (its x is not read).  Products of 16-bit numbers, sums in fp32: the
+ * inner sums are held in fp32 and go into the outer ones to 17 bits or more (24
+ * for bf16 x with fp32 y, 22 for fp16 x), and out is rounded to y's type once. */
+typedef struct archead_adapters {
+  const void* a;            /* x's type: adapter i's a_i [R, K] at i * a_adapter, rows a_row apart */
+  const void* b;            /* x's type: b_i [N, R] at i * b_adapter, rows b_row apart (all in elements) */
+  const float* scales;      /* device fp32 [n], or NULL for 1 */
+  const int32_t* ranks;     /* device int32 [n], or NULL for R: of a_i the first ranks[i] rows count and of
+                               b_i the first ranks[i] columns (clamped to [0, R]); the rest is not used, whatever it holds */
+  int64_t n, R;             /* adapters; 0 <= R <= 256 */
+  int64_t a_adapter, a_row, b_adapter, b_row;
+} archead_adapters;
+
+/* Bytes of workspace archead_adapters_add needs (0 where a size is < 1 or out
+ * of range: then there is nothing to compute, or the call is refused). */
+size_t archead_adapters_workspace_bytes(int64_t M, int64_t K, int64_t R, int64_t n);
+
+/*   y    fp32, bf16 or fp16 [M, ldy] device, ldy >= N;  out the same type
+ *        [M, ldo], ldo >= N: y itself (then ldo == ldy), or sharing no memory
+ *        with an input
+ *   x    bf16 or fp16 [M, ldx] device, ldx >= K
+ *   ids  device int32 or int64 [M], in any order
+ *   ws   device scratch of archead_adapters_workspace_bytes(M, K, R, n) bytes,
+ *        256-byte aligned, contents on entry do not matter
+ *   stream  hipStream_t (NULL = the default stream); asynchronous
+ * Pointers are aligned to their element size; K and R that are multiples of 8
+ * are fastest.  Results are reproducible.  `adapters` is read before the call
+ * returns.  M = 0 or N = 0 is a no-op; n = 0, R = 0 or K = 0 adds nothing.
+ * ARCHEAD_E_INVALID_ARG for a null pointer, a size < 0, M or K >= 2^31, N > 2^23,
+ * n >= 2^30, a leading dimension or row stride too small, a stride < 0 or above 2^40, or a
+ * dtype not listed; ARCHEAD_E_UNSUPPORTED for R > 256; ARCHEAD_E_MISALIGNED;
+ * ARCHEAD_E_WORKSPACE; ARCHEAD_E_HIP when a launch fails. */
+archead_status archead_adapters_add(const void* y, archead_dtype y_dtype, int64_t ldy, const void* x,
+                                    archead_dtype x_dtype, int64_t ldx,
+                                    const archead_adapters* adapters, const void* ids,
+                                    archead_dtype ids_dtype, int64_t M, int64_t N, int64_t K,
+                                    void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Beam search: the choice of the next hypotheses, and the states they
  * continue.  B sequences of K beams each; row b * K + k belongs to beam k of
  * sequence b.

@@ -12,6 +12,7 @@ from .archead import (  # noqa: F401
     beam_select,
     build_head,
     PackedHead,
+    adapters_add,
     logit_fidelity,
     lib,
     matmul_i8,

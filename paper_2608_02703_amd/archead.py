@@ -72,6 +72,12 @@ class StateLayout(ctypes.Structure):
         "dst_row", "dst_outer", "dst_pos")]
 
 
+class AdaptersDesc(ctypes.Structure):
+    """archead_adapters: the low-rank pairs of many requests."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("a", "b", "scales", "ranks")] +
+                [(n, ctypes.c_int64) for n in ("n", "R", "a_adapter", "a_row", "b_adapter", "b_row")])
+
+
 _SIGS = {
     "archead_validate_desc": (ctypes.c_int, [ctypes.POINTER(Desc)]),
     "archead_create": (ctypes.c_int, [ctypes.POINTER(Desc), ctypes.POINTER(Ptrs),
@@ -129,6 +135,13 @@ _SIGS = {
                                         ctypes.c_int, ctypes.c_float, ctypes.c_double, ctypes.c_void_p,
                                         ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                         ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]),
+    "archead_adapters_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                                           ctypes.c_int64]),
+    "archead_adapters_add": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_int, ctypes.c_int64, ctypes.POINTER(AdaptersDesc),
+                                            ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                            ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_size_t, ctypes.c_void_p]),
     "archead_beam_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
     "archead_beam_select": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64,
                                            ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
@@ -472,6 +485,55 @@ def rms_norm_i8(x, weight, eps=1e-6, residual=None, offset=0.0, normed=False, co
     out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if normed is True else None if normed is False else normed
     total = _norm_call(x, weight, eps, residual, offset, total, out, codes, scales)
     return (codes, scales) + (() if residual is None else (total,)) + (() if out is None else (out,))
+
+
+def _factors(t, what, gpu, dtype):
+    """Steps of the adapters and of the rows of a [n, rows, columns] tensor."""
+    if t.get_device() != gpu or not t.is_cuda:
+        raise ValueError(f"{what} must be on GPU {gpu}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{what} must be 3-D with unit column stride")
+    return (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else t.shape[2])
+
+
+def adapters_add(y, x, a, b, ids, scales=None, ranks=None, out=None, ws=None):
+    """y + scales[i] * (x @ a[i].T) @ b[i].T with i = ids[m] for each token m,
+    and y where ids[m] lies outside [0, n): low-rank adapters of many requests
+    beside a shared projection (archead_adapters_add).  y: float32, bfloat16 or
+    float16 [M, N]; x: bfloat16 or float16 [M, K]; a [n, R, K] and b [n, N, R] of
+    x's type, R <= 256; ids: int32 or int64 [M]; scales: float32 [n] or None;
+    ranks: int32 [n], adapters of fewer than R, or None.  out may be y."""
+    import torch
+    gpu = _gpu_of(y, "y")
+    ldy = _matrix(y, "y", gpu)
+    ldx = _matrix(x, "x", gpu)
+    code, xcode = _float_code(y.dtype, "y"), _float_code(x.dtype, "x")
+    (M, N), K = y.shape, x.shape[1]
+    a_ad, a_row = _factors(a, "a", gpu, x.dtype)
+    b_ad, b_row = _factors(b, "b", gpu, x.dtype)
+    n, R = a.shape[:2]
+    if x.shape[0] != M or a.shape[2] != K or b.shape != (n, N, R):
+        raise ValueError("x must be [M, K], a [n, R, K] and b [n, N, R] with y [M, N]")
+    _dense(ids, "ids", gpu, (torch.int64, torch.int32), (M,))
+    if scales is not None:
+        _dense(scales, "scales", gpu, (torch.float32,), (n,))
+    if ranks is not None:
+        _dense(ranks, "ranks", gpu, (torch.int32,), (n,))
+    if out is None:
+        out, ldo = torch.empty((M, N), dtype=y.dtype, device=y.device), N
+    else:
+        ldo = ldy if out is y else _matrix(out, "out", gpu, y.dtype, (M, N))
+    L = lib()
+    if ws is None:
+        ws = torch.empty(max(L.archead_adapters_workspace_bytes(M, K, R, n), 256), dtype=torch.uint8, device=y.device)
+    elif ws.get_device() != gpu or not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous uint8 tensor on the same GPU")
+    desc = AdaptersDesc(a.data_ptr(), b.data_ptr(), _ptr(scales), _ptr(ranks), n, R, a_ad, a_row, b_ad, b_row)
+    _launch(gpu, L.archead_adapters_add, y.data_ptr(), code, ldy, x.data_ptr(), xcode, ldx, desc, ids.data_ptr(),
+            I64 if ids.dtype == torch.int64 else I32, M, N, K, out.data_ptr(), ldo, ws.data_ptr(), ws.numel())
+    return out
 
 
 def _beam_call(gpu, device, scores, n, finished, end_token, ws, ws_bytes, call):

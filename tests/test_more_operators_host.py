@@ -50,3 +50,46 @@ def test_python_refuses_host_tensors():
         lib.rms_norm(x, w)
     with pytest.raises(ValueError):
         lib.rms_norm_i8(x, w)
+
+
+def _adapters(L, **kw):
+    a = dict(y=P, yt=ab.BF16, ldy=32, x=P, xt=ab.BF16, ldx=64, ad=True, ids=P, it=ab.I64, M=2, N=32, K=64, out=2 * P,
+             ldo=32, ws=P, wsb=1 << 20)
+    d = dict(a=P, b=P, scales=P, ranks=P, n=3, R=16, a_ad=1024, a_row=64, b_ad=512, b_row=16)
+    d.update({k: v for k, v in kw.items() if k in d})
+    a.update({k: v for k, v in kw.items() if k in a})
+    a["ad"] = ab.AdaptersDesc(*d.values()) if a["ad"] else None
+    return L.archead_adapters_add(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(M=0), ab.OK), (dict(N=0), ab.OK), (dict(n=0, out=P), ab.OK), (dict(R=0, out=P, a=None, b=None), ab.OK),
+    (dict(K=0, out=P, x=None, ws=None), ab.OK),
+    (dict(yt=ab.I8), ab.E_INVALID_ARG), (dict(xt=ab.F32), ab.E_INVALID_ARG), (dict(it=ab.F32), ab.E_INVALID_ARG),
+    (dict(ad=False), ab.E_INVALID_ARG), (dict(M=-1), ab.E_INVALID_ARG), (dict(M=2 ** 31), ab.E_INVALID_ARG),
+    (dict(N=2 ** 23 + 1, ldy=2 ** 24, ldo=2 ** 24), ab.E_INVALID_ARG), (dict(K=-1), ab.E_INVALID_ARG),
+    (dict(n=-1), ab.E_INVALID_ARG), (dict(n=2 ** 30), ab.E_INVALID_ARG), (dict(R=-1), ab.E_INVALID_ARG),
+    (dict(R=257, b_row=300), ab.E_UNSUPPORTED), (dict(ldy=31), ab.E_INVALID_ARG), (dict(ldo=31), ab.E_INVALID_ARG),
+    (dict(ldx=63), ab.E_INVALID_ARG), (dict(a_ad=-1), ab.E_INVALID_ARG), (dict(a_row=63), ab.E_INVALID_ARG),
+    (dict(b_ad=2 ** 41), ab.E_INVALID_ARG), (dict(b_row=15), ab.E_INVALID_ARG), (dict(y=None), ab.E_INVALID_ARG),
+    (dict(x=None), ab.E_INVALID_ARG), (dict(a=None), ab.E_INVALID_ARG), (dict(b=None), ab.E_INVALID_ARG),
+    (dict(ids=None), ab.E_INVALID_ARG), (dict(out=None), ab.E_INVALID_ARG), (dict(ws=None), ab.E_INVALID_ARG),
+    (dict(out=P, ldo=40), ab.E_INVALID_ARG), (dict(y=P + 1), ab.E_MISALIGNED), (dict(x=P + 1), ab.E_MISALIGNED),
+    (dict(a=P + 1), ab.E_MISALIGNED), (dict(b=P + 1), ab.E_MISALIGNED), (dict(out=P + 1), ab.E_MISALIGNED),
+    (dict(ids=P + 4), ab.E_MISALIGNED), (dict(scales=P + 2), ab.E_MISALIGNED), (dict(ranks=P + 2), ab.E_MISALIGNED),
+    (dict(yt=ab.F32, y=P + 2), ab.E_MISALIGNED), (dict(ws=P + 16), ab.E_MISALIGNED), (dict(wsb=64), ab.E_WORKSPACE),
+])
+def test_adapters_refusals(L, kw, status):
+    assert _adapters(L, **kw) == status, L.archead_last_error()
+
+
+def test_adapters_workspace_bytes(L):
+    f = L.archead_adapters_workspace_bytes
+    assert f(0, 64, 16, 2) == f(2, 0, 16, 2) == f(2, 64, 0, 2) == f(2, 64, 16, 0) == f(2, 64, 257, 2) == 0
+    assert f(1, 64, 16, 2) % 256 == 0 and f(8192, 4096, 64, 8) < 8192 * 4096
+
+
+def test_python_refuses_host_adapters():
+    y, x = torch.zeros(2, 8), torch.zeros((2, 4), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        lib.adapters_add(y, x, x[None], x[None], torch.zeros(2, dtype=torch.int64))
