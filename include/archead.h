@@ -655,6 +655,56 @@ archead_status archead_rms_norm(const void* x, archead_dtype dtype, int64_t M, i
                                 float* scales, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Softmax cross entropy of a dense bf16 head (the one that a packed head is
+ * built from) with its gradients, a piece of the vocabulary at a time: no
+ * [M, V] array of logits is kept.  For a token m < M with target y in [0, V):
+ *   logit[v] = sum_i x[m, i] w[v, i]       products exact, sums in fp32
+ *   lse[m]   = log sum_v exp(logit[v]),    loss[m] = lse[m] - logit[y]
+ *   G[m, v]  = grad[m] (exp(logit[v] - lse[m]) - [v = y])
+ *   dx[m, :] = sum_v G[m, v] w[v, :],      dw[v, :] = sum_m G[m, v] x[m, :]
+ * grad[m] is what the loss of token m counts for in the whole (1 / M for a
+ * mean).  G is rounded to bf16 for its products (its entries, and
+ * exponentials, below 2^-126 count as 0), whose sums are fp32; dx and dw are
+ * rounded to bf16 once.  A token whose target lies outside [0, V) (say
+ * -100) has loss 0, lse 0 and dx 0 and adds nothing to dw, whatever its row of x
+ * and its grad hold; it costs no products.  A token whose logits hold a NaN or +inf gets
+ * NaN. */
+
+/* Bytes of device workspace of the calls below (grad: 0 for archead_head_loss,
+ * 1 for archead_head_loss_grad; 0 for M < 1 or sizes that the calls refuse).
+ * w and ldw as in the call: rows of w that are not whole 128-byte pieces at
+ * 16-byte aligned places (d % 64, ldw % 8, ldw > 2^20) are copied there by pieces. */
+size_t archead_head_loss_workspace_bytes(int64_t M, int64_t V, int64_t d, const void* w,
+                                         int64_t ldw, int grad);
+
+/*   x        bf16 [M, ldx] device, ldx >= d;  w  bf16 [V, ldw] device, ldw >= d
+ *   targets  device int32 or int64 [M] (tgt_dtype ARCHEAD_I32 / ARCHEAD_I64)
+ *   loss, lse  device fp32 [M]
+ *   ws       device scratch of archead_head_loss_workspace_bytes(...) bytes,
+ *            256-byte aligned, contents on entry do not matter
+ *   stream   hipStream_t (NULL = the default stream); asynchronous
+ * Outputs share no memory with inputs.  Results are reproducible.  M = 0 is a
+ * no-op.  ARCHEAD_E_INVALID_ARG for a null pointer, M < 0, V < 1, d < 1, a
+ * leading dimension < d or a dtype not listed; ARCHEAD_E_UNSUPPORTED for
+ * M > 2^20, V > 2^22 or d > 16384; ARCHEAD_E_MISALIGNED; ARCHEAD_E_WORKSPACE;
+ * ARCHEAD_E_HIP when a launch fails. */
+archead_status archead_head_loss(const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                 const void* targets, archead_dtype tgt_dtype, int64_t M, int64_t V,
+                                 int64_t d, float* loss, float* lse, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* The gradients, with lse from archead_head_loss on the same x, w and targets.
+ *   grad  device fp32 [M]
+ *   dx    bf16 [M, lddx] device or NULL;  dw  bf16 [V, lddw] device or NULL
+ *         (a frozen head); leading dimensions >= d, not both NULL
+ * M = 0 sets dw to zeros.  The rest as archead_head_loss. */
+archead_status archead_head_loss_grad(const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                      const void* targets, archead_dtype tgt_dtype, const float* lse,
+                                      const float* grad, int64_t M, int64_t V, int64_t d, void* dx,
+                                      int64_t lddx, void* dw, int64_t lddw, void* ws,
+                                      size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Low-rank adapters of many requests at once, beside a projection that they
  * share (archead_matmul_i8, a head, any other product): for m < M, with i =
  * ids[m],

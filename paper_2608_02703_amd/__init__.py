@@ -13,6 +13,8 @@ from .archead import (  # noqa: F401
     build_head,
     PackedHead,
     adapters_add,
+    head_loss,
+    head_loss_grad,
     logit_fidelity,
     lib,
     matmul_i8,

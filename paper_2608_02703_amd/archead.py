@@ -142,6 +142,17 @@ _SIGS = {
                                             ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
                                             ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                             ctypes.c_size_t, ctypes.c_void_p]),
+    "archead_head_loss_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                                            ctypes.c_void_p, ctypes.c_int64, ctypes.c_int]),
+    "archead_head_loss": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                         ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                         ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_size_t, ctypes.c_void_p]),
+    "archead_head_loss_grad": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                              ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                              ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                              ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                              ctypes.c_size_t, ctypes.c_void_p]),
     "archead_beam_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
     "archead_beam_select": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64,
                                            ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
@@ -534,6 +545,65 @@ def adapters_add(y, x, a, b, ids, scales=None, ranks=None, out=None, ws=None):
     _launch(gpu, L.archead_adapters_add, y.data_ptr(), code, ldy, x.data_ptr(), xcode, ldx, desc, ids.data_ptr(),
             I64 if ids.dtype == torch.int64 else I32, M, N, K, out.data_ptr(), ldo, ws.data_ptr(), ws.numel())
     return out
+
+
+def _loss_call(x, w, targets, ws, grad):
+    """Checks of a head loss's inputs: (gpu, leading arguments, M, V, d, ws)."""
+    import torch
+    gpu = _gpu_of(x, "x")
+    ldx = _matrix(x, "x", gpu, torch.bfloat16)
+    ldw = _matrix(w, "w", gpu, torch.bfloat16)
+    (M, d), V = x.shape, w.shape[0]
+    if w.shape[1] != d:
+        raise ValueError("x and w must have the same number of columns")
+    _dense(targets, "targets", gpu, (torch.int64, torch.int32), (M,))
+    code = I64 if targets.dtype == torch.int64 else I32
+    if ws is None:
+        need = lib().archead_head_loss_workspace_bytes(M, V, d, w.data_ptr(), ldw, grad)
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
+    elif ws.get_device() != gpu or not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous uint8 tensor on the same GPU")
+    return gpu, (x.data_ptr(), ldx, w.data_ptr(), ldw, targets.data_ptr(), code), M, V, d, ws
+
+
+def head_loss(x, w, targets, loss=None, lse=None, ws=None):
+    """Softmax cross entropy of the dense head w (bfloat16 [V, d]) on the hidden
+    states x (bfloat16 [M, d]) without an [M, V] array of logits
+    (archead_head_loss): returns (loss float32 [M], lse float32 [M]), both 0 where
+    targets (int32 or int64 [M]) lie outside [0, V)."""
+    import torch
+    gpu, args, M, V, d, ws = _loss_call(x, w, targets, ws, 0)
+    loss = torch.empty(M, dtype=torch.float32, device=x.device) if loss is None else loss
+    lse = torch.empty(M, dtype=torch.float32, device=x.device) if lse is None else lse
+    _dense(loss, "loss", gpu, (torch.float32,), (M,))
+    _dense(lse, "lse", gpu, (torch.float32,), (M,))
+    _launch(gpu, lib().archead_head_loss, *args, M, V, d, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel())
+    return loss, lse
+
+
+def head_loss_grad(x, w, targets, lse, grad, dx=True, dw=True, ws=None):
+    """The gradients of sum(grad * loss) of head_loss, lse its second result and
+    grad float32 [M] (archead_head_loss_grad): returns (dx bfloat16 [M, d], dw
+    bfloat16 [V, d]).  dx and dw are True, a tensor for the result, or False where it is
+    not wanted (then None is returned).  A training step goes on with
+    x.backward(dx) and w.grad = dw."""
+    import torch
+    gpu, args, M, V, d, ws = _loss_call(x, w, targets, ws, 1)
+    _dense(lse, "lse", gpu, (torch.float32,), (M,))
+    _dense(grad, "grad", gpu, (torch.float32,), (M,))
+
+    def result(t, what, rows):
+        if t is None or t is False:
+            return None, d
+        if t is True:
+            return torch.empty((rows, d), dtype=torch.bfloat16, device=x.device), d
+        return t, _matrix(t, what, gpu, torch.bfloat16, (rows, d))
+    (dx, lddx), (dw, lddw) = result(dx, "dx", M), result(dw, "dw", V)
+    if dx is None and dw is None:
+        raise ValueError("dx or dw must be wanted")
+    _launch(gpu, lib().archead_head_loss_grad, *args, lse.data_ptr(), grad.data_ptr(), M, V, d, _ptr(dx), lddx, _ptr(dw), lddw,
+            ws.data_ptr(), ws.numel())
+    return dx, dw
 
 
 def _beam_call(gpu, device, scores, n, finished, end_token, ws, ws_bytes, call):

@@ -1,0 +1,53 @@
+// archead_head_loss, archead_head_loss_grad: sizes, workspace and the tile
+// kernels' arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace archead {
+namespace loss {
+
+constexpr int kTileJ = 256;        // columns of a tile
+constexpr int kStageK = 64;        // k of a stage
+constexpr int kRowPad = 256;       // live tokens are padded with zero rows up to a multiple of this
+
+// The products, out[i, j] = sum_k: 
+//   kStats   i token, j vocabulary row, k of d: a tile's largest logit and sum of
+//            exponentials per token, and the target's logit
+//   kGrad    the same logits, as G = g (exp(l - lse) - [j = target]) in bf16
+//   kHidden  i token, j of d, k vocabulary row: sums of G w into fp32
+//   kHead    i vocabulary row, j of d, k token: rows of G^T x in bf16
+enum Op { kStats, kGrad, kHidden, kHead };
+
+struct TileArgs {
+  const uint16_t* a;       // operand of i: [i][k], for kHead [k][i]
+  const uint16_t* b;       // operand of j: [j][k], for kHidden and kHead [k][j]
+  int64_t a_ld, b_ld;      // elements between rows
+  int64_t rows;            // kHead: i; else of tokens at most (the device's count says)
+  int64_t cols;            // j
+  int64_t depth;           // k (kHead: at most, the device's count says)
+  const int32_t* count;    // live tokens
+  int64_t v0;              // first vocabulary row of the piece
+  // kStats
+  float2* part;            // [token][n_part] (largest, sum)
+  int64_t n_part, part0;   // tiles of the vocabulary; the piece's first one
+  float* at_target;        // [token]
+  // kGrad
+  const int32_t* target;   // [token]
+  const float* lse;        // [token]
+  const float* g;          // [token]
+  uint16_t* out;           // kGrad: G [token][out_ld]; kHead: dw
+  int64_t out_ld;
+  // kHidden
+  float* sums;             // [split][row][sum_ld]
+  int64_t sum_ld, split_step;
+  int splits;              // parts of k
+  bool add;                // to what sums holds
+};
+
+// tiles of ti x 256, ti = 64, 128 or 256 (kHead: 256)
+hipError_t launch_tiles(Op op, int ti, const TileArgs& g, hipStream_t s);
+
+}  // namespace loss
+}  // namespace archead

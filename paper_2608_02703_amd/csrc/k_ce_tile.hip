@@ -1,0 +1,411 @@
+// Tiles of the dense head's products: logits and their statistics, the logits'
+// gradient, and the gradients of hidden states and head.
+#include <algorithm>
+
+#include "dev_common.cuh"
+#include "dev_rows.cuh"
+#include "head_loss.h"
+
+namespace {
+
+using namespace archead::rows;
+using namespace archead::loss;
+
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRasterI = 8;        // tiles of i in a raster group
+
+template <int OP, int TI>
+struct Geom {
+  static constexpr bool AT = OP == kHead, BT = OP == kHidden || OP == kHead;   // operands whose rows are k
+  static constexpr int WI = TI >= 128 ? 2 : 1, WJ = 8 / WI, NW = 8;             // waves along i, j
+  static constexpr int NI = TI / WI / 32, NJ = kTileJ / WJ / 32;                // blocks of 32 x 32 of a wave
+  static constexpr int NS = 2;                                                  // stages in LDS
+  static constexpr int ABYTES = TI * kStageK * 2, BBYTES = kTileJ * kStageK * 2, STAGE = ABYTES + BBYTES;
+  static constexpr int LA = ABYTES / 1024 / NW, LB = BBYTES / 1024 / NW;        // loads of a wave and stage
+  static constexpr int OROW = kTileJ * 2 + 16;                                  // a row of 16-bit outputs in LDS, padded
+  static constexpr int RED = OP == kStats ? WJ * TI * 8 : 0;
+  static constexpr int BODY = std::max(NS * STAGE, OP == kGrad || OP == kHead ? TI * OROW : RED);
+  static constexpr int LDS = BODY;
+  static_assert(LDS <= 160 * 1024, "LDS budget");
+  static_assert(!AT || TI == 256, "rows of k are 256 wide");
+};
+
+// After each of the first products of a K-step a share of its R LDS reads; of V
+// loads to LDS after all of them.  Without it the compiler puts the reads right
+// before their use.
+template <int R, int V, int P, int I = 0>
+__device__ __forceinline__ void spread() {
+  if constexpr (I < P) {
+    constexpr int H = P * 3 / 4 > 0 ? P * 3 / 4 : 1;
+    constexpr int r = I < H ? R * (I + 1) / H - R * I / H : 0, v = V * (I + 1) / P - V * I / P;
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);   // products
+    if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    if constexpr (v > 0) __builtin_amdgcn_sched_group_barrier(0x10, v, 0);
+    spread<R, V, P, I + 1>();
+  } else {
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// 16 bytes a lane, at voff + soff of a buffer, to LDS
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, lds_u8* to, uint32_t voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, reinterpret_cast<__attribute__((address_space(3))) void*>(to), 16, voff, soff, 0, 0);
+}
+
+// One operand's way to LDS and into registers.  T false: rows of the operand, 64 k =
+// 128 bytes each, their 16-byte units swizzled so that eight rows' reads of one unit
+// fall on eight different bank groups.  T true: rows of k, 256 columns = 512 bytes
+// each; a group of 16 lanes reads four rows of 16 columns and gets them transposed,
+// so a lane has four k of its column.  There the 64-byte parts of a row are swizzled
+// by its place among four: the four rows of a read then lie in different banks.
+template <bool T, int ROWS, int LOADS, int BLOCKS>
+struct Operand {
+  const uint16_t* base;
+  int64_t ld, krows;       // krows (T): rows there are
+  int cols;                // T: columns there are, from the tile's first on
+  int bytes;               // T false: from base to the end of the last row
+  uint32_t off[LOADS];
+  uint32_t at[4];          // of a lane's reads
+
+  // a load's place in LDS of this lane: row and 16-byte unit of the source
+  static __device__ __forceinline__ void place(int i, int wid, int lane, int& r, int& u) {
+    const int o = (wid * LOADS + i) * 1024 + 16 * lane;
+    if constexpr (T) {
+      r = o / 512;
+      u = (o % 512 / 16) ^ (4 * (r & 3));
+    } else {
+      r = o / 128;
+      u = (o % 128 / 16) ^ swz_x(r);
+    }
+  }
+  // T false: `first` row of `all`; T true: `first` column of `all`, krows rows of k
+  __device__ __forceinline__ void begin(const uint16_t* p, int64_t ld_, int64_t first, int64_t all, int64_t k, int wid, int lane) {
+    ld = ld_;
+    if constexpr (T) {
+      base = p + first;
+      krows = k;
+      cols = int(all - first < kTileJ ? all - first : kTileJ);
+    } else {
+      base = p + first * ld;
+      const int there = int(all - first < ROWS ? all - first : ROWS);
+      bytes = int(((there - 1) * ld + k) * 2);
+      cols = there;
+    }
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      int r, u;
+      place(i, wid, lane, r, u);
+      off[i] = T ? uint32_t(r * ld * 2) + 2 * min(8 * u, (cols - 1) & ~7) : uint32_t(min(r, cols - 1) * ld * 2) + 16 * u;
+    }
+  }
+  __device__ __forceinline__ void issue(lds_u8* to, int64_t k0, int wid, int lane) {
+    if constexpr (T) {
+      const int left = int(krows - k0 < kStageK ? krows - k0 : kStageK);
+      const auto r64 = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + k0 * ld), 0,
+                                                         int(((left - 1) * ld + ((cols + 7) & ~7)) * 2), kBufferWord3);
+      if (left == kStageK) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          load_lds(r64, to + (wid * LOADS + i) * 1024, off[i], 0);
+      } else {   // rows past the last repeat it (the other operand has zeros there)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          int r, u;
+          place(i, wid, lane, r, u);
+          load_lds(r64, to + (wid * LOADS + i) * 1024, uint32_t(min(r, left - 1) * ld * 2) + 2 * min(8 * u, (cols - 1) & ~7), 0);
+        }
+      }
+    } else {
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, bytes, kBufferWord3);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        load_lds(rsrc, to + (wid * LOADS + i) * 1024, off[i], int(k0 * 2));
+    }
+  }
+  // this wave's reads begin at row (column) `first` of the tile
+  __device__ __forceinline__ void aim(int first, int lane) {
+    const int lr = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (T) {   // of block i
+        const int row = (lane >> 2) & 3, unit = (first + 32 * i) / 8 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        at[i] = (8 * h + row) * 512 + 16 * (unit ^ (4 * row)) + 8 * (lane & 1);
+      } else {             // of K-step i
+        at[i] = (first + lr) * 128 + 16 * ((2 * i + h) ^ swz_x(lr));
+      }
+    }
+  }
+  __device__ __forceinline__ void read(b16x8 (&to)[BLOCKS], const lds_u8* from, int ks) const {
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+      if constexpr (T) {
+        auto half = [&](int j) {
+          return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(from + at[i] + (16 * ks + 4 * j) * 512));
+        };
+        const s16x4 lo = half(0), hi = half(1);
+        to[i] = __builtin_bit_cast(b16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      } else {
+        to[i] = lds_load<b16x8>(from + at[ks] + 32 * i * 128);
+      }
+    }
+  }
+  static constexpr int kReads = BLOCKS * (T ? 2 : 1);
+};
+
+template <int OP, int TI>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ce_tile(TileArgs g) {
+  using G = Geom<OP, TI>;
+  constexpr int NI = G::NI, NJ = G::NJ, NS = G::NS;
+  extern __shared__ __align__(16) uint8_t ce_lds[];
+  lds_u8* const L = (lds_u8*)ce_lds;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wi = wid / G::WJ, wj = wid % G::WJ;
+  const int live = *g.count;
+  const int64_t rows = OP == kHead ? g.rows : int64_t(live);
+  const int64_t depth = OP == kHead ? (int64_t(live) + kStageK - 1) / kStageK * kStageK : g.depth;
+
+  // workgroups go to the 8 XCDs in turn; each XCD takes a contiguous run of the
+  // order that walks groups of kRasterI tiles of i along j
+  const int i_tiles = int((rows + TI - 1) / TI), j_tiles = int((g.cols + kTileJ - 1) / kTileJ);
+  const int splits = OP == kHidden ? g.splits : 1;
+  const int n_all = i_tiles * j_tiles * splits, per_xcd = (n_all + 7) / 8;
+  const int lin = int(blockIdx.x & 7) * per_xcd + int(blockIdx.x >> 3);
+  if (int(blockIdx.x >> 3) >= per_xcd || lin >= n_all) return;
+  const int tile = lin % (i_tiles * j_tiles), split = lin / (i_tiles * j_tiles);
+  const int gsz = kRasterI * j_tiles, rg = tile / gsz, first = rg * kRasterI;
+  const int gi = min(i_tiles - first, kRasterI), within = tile - rg * gsz;
+  const int64_t i0 = int64_t(first + within % gi) * TI, j0 = int64_t(within / gi) * kTileJ;
+
+  const int all_stages = int((depth + kStageK - 1) / kStageK);
+  const int s0 = int(int64_t(all_stages) * split / splits), s1 = int(int64_t(all_stages) * (split + 1) / splits);
+  const int stages = s1 - s0;
+
+  Operand<G::AT, TI, G::LA, NI> a;
+  Operand<G::BT, kTileJ, G::LB, NJ> b;
+  a.begin(g.a, g.a_ld, i0, OP == kHead ? (rows + 255) / 256 * 256 : rows, int64_t(all_stages) * kStageK, wid, lane);
+  b.begin(g.b, g.b_ld, j0, g.cols, OP == kHidden ? g.depth : depth, wid, lane);
+  a.aim(wi * NI * 32, lane);
+  b.aim(wj * NJ * 32, lane);
+  auto issue = [&](int s) {
+    lds_u8* const to = L + (s % NS) * G::STAGE;
+    const int64_t k0 = int64_t(s0 + s) * kStageK;
+    a.issue(to, k0, wid, lane);
+    b.issue(to + G::ABYTES, k0, wid, lane);
+  };
+  b16x8 A[2][NI], B[2][NJ];
+  f32x16 acc[NI][NJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+  auto read = [&](int to, int s, int ks) {
+    const lds_u8* const from = L + (s % NS) * G::STAGE;
+    a.read(A[to], from, ks);
+    b.read(B[to], from + G::ABYTES, ks);
+  };
+  auto multiply = [&](int of) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(B[of][j], A[of][i], acc[i][j], 0, 0, 0);
+  };
+  constexpr int kReads = decltype(a)::kReads + decltype(b)::kReads, P = NI * NJ;
+  // A wave reads the operands of a K-step (16 k) during the step before.  Before the
+  // last step of a stage all its reads are done, so there the waves meet, once a
+  // stage: the next stage has landed, its first operands are read and the loads of
+  // the one after overwrite this one, all under the last step's products.
+  if (stages > 0) {
+    issue(0);
+    if (stages > 1) issue(1);
+    wait_loads_barrier<0>();
+    read(0, 0, 0);
+#pragma unroll 1
+    for (int s = 0; s < stages; ++s) {
+      __builtin_amdgcn_sched_barrier(0);
+      read(1, s, 1);
+      multiply(0);
+      spread<kReads, 0, P>();
+      read(0, s, 2);
+      multiply(1);
+      spread<kReads, 0, P>();
+      read(1, s, 3);
+      multiply(0);
+      spread<kReads, 0, P>();
+      wait_loads_barrier<0>();
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + NS < stages) issue(s + NS);
+      if (s + 1 < stages) read(0, s + 1, 0);
+      multiply(1);
+    }
+  }
+
+  // ---- outputs.  A lane's results: row i = lr of a block, columns 8 (r / 4) + 4 h + r % 4
+  const int64_t jw = j0 + wj * NJ * 32;   // this wave's first column
+  if constexpr (OP == kStats) {
+    float2* const red = reinterpret_cast<float2*>(ce_lds);   // [WJ][TI]
+    __syncthreads();
+    const bool whole = j0 + kTileJ <= g.cols;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int row = wi * NI * 32 + 32 * i + lr;
+      const int64_t token = i0 + row;
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (jw + 32 * j + 8 * (r / 4) + 4 * h + r % 4 >= g.cols) acc[i][j][r] = -INFINITY;
+      }
+      float top = -INFINITY, sum = 0;
+      bool odd = false;   // a NaN among them
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          top = fmaxf(top, acc[i][j][r]);
+          odd |= acc[i][j][r] != acc[i][j][r];
+        }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (top > -INFINITY) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - top) * kLog2e);
+      }
+      if (odd) sum = NAN;
+      sum += __shfl_xor(sum, 32);
+      if (h == 0) red[wj * TI + row] = float2{top, sum};
+      const int64_t y = token < live ? g.target[token] - g.v0 - jw : -1;   // of this wave's columns
+      if (y >= 0 && y < NJ * 32 && (y >> 2 & 1) == h) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (y == 32 * j + 8 * (r / 4) + 4 * h + r % 4) g.at_target[token] = acc[i][j][r];
+      }
+    }
+    __syncthreads();
+    if (tid < TI && i0 + tid < live) {
+      float top = -INFINITY, sum = 0;
+#pragma unroll
+      for (int w = 0; w < G::WJ; ++w) top = fmaxf(top, red[w * TI + tid].x);
+#pragma unroll
+      for (int w = 0; w < G::WJ; ++w) {
+        const float2 p = red[w * TI + tid];
+        sum += p.x == top ? p.y : p.y * __builtin_amdgcn_exp2f((p.x - top) * kLog2e);
+      }
+      g.part[(i0 + tid) * g.n_part + g.part0 + j0 / kTileJ] = float2{top, sum};
+    }
+  } else if constexpr (OP == kHidden) {
+    float* const base = g.sums + split * g.split_step;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      float* const row = base + (i0 + wi * NI * 32 + 32 * i + lr) * g.sum_ld;   // (rows are padded to whole tiles)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int64_t c = jw + 32 * j + 2 * r + 4 * h;
+          if (c >= g.sum_ld) continue;   // (a multiple of 64)
+          f32x4v v{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+          f32x4v* const p = reinterpret_cast<f32x4v*>(row + c);
+          if (g.add) v += *p;
+          *p = v;
+        }
+    }
+  } else {
+    // 16-bit rows through LDS, so that 32 lanes store what lies together
+    __syncthreads();
+    const int64_t cols = g.cols;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int row = wi * NI * 32 + 32 * i + lr;
+      const int64_t token = i0 + row;
+      float lse = 0, gr = 0;
+      int64_t y = -1;
+      if constexpr (OP == kGrad) {
+        if (token < live) {
+          lse = g.lse[token];
+          gr = g.g[token];
+          y = g.target[token] - g.v0 - jw;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          f32x4v v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = acc[i][j][r + e];
+            if constexpr (OP == kGrad) {
+              const int c = 32 * j + 2 * r + 4 * h + e;
+              float p = __builtin_amdgcn_exp2f((v[e] - lse) * kLog2e);
+              if (y == c) p -= 1.f;
+              v[e] = token < live && jw + c < cols ? p * gr : 0.f;
+            }
+          }
+          const b16x4 o = __builtin_convertvector(v, b16x4);
+          *reinterpret_cast<b16x4*>(ce_lds + row * G::OROW + (wj * NJ * 32 + 32 * j + 2 * r + 4 * h) * 2) = o;
+        }
+    }
+    __syncthreads();
+    for (int row = tid >> 5; row < TI; row += 16) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(ce_lds + row * G::OROW + 16 * (tid & 31));
+      const int64_t j = j0 + 8 * (tid & 31);
+      uint16_t* const p = g.out + (i0 + row) * g.out_ld + j;
+      if constexpr (OP == kGrad) {   // (G has whole tiles)
+        *reinterpret_cast<u32x4*>(p) = v;
+      } else if (i0 + row < rows && j < cols) {
+        if (j + 8 <= cols) {
+          store_any(p, v);
+        } else {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (j + e < cols) p[e] = uint16_t(w[e / 2] >> (16 * (e & 1)));
+        }
+      }
+    }
+  }
+}
+
+template <int OP, int TI>
+hipError_t launch(const TileArgs& g, hipStream_t s) {
+  const int64_t i_tiles = (g.rows + TI - 1) / TI, j_tiles = (g.cols + kTileJ - 1) / kTileJ;
+  const int64_t n = i_tiles * j_tiles * (OP == kHidden ? g.splits : 1);
+  return launch_kernel_lds(k_ce_tile<OP, TI>, dim3(unsigned((n + 7) / 8 * 8)), dim3(512), Geom<OP, TI>::LDS, s, g);
+}
+
+template <int OP>
+hipError_t launch_op(int ti, const TileArgs& g, hipStream_t s) {
+  return ti == 256 ? launch<OP, 256>(g, s) : ti == 128 ? launch<OP, 128>(g, s) : launch<OP, 64>(g, s);
+}
+
+}  // namespace
+
+namespace archead {
+namespace loss {
+
+hipError_t launch_tiles(Op op, int ti, const TileArgs& g, hipStream_t s) {
+  switch (op) {
+    case kStats: return launch_op<kStats>(ti, g, s);
+    case kGrad: return launch_op<kGrad>(ti, g, s);
+    case kHidden: return launch_op<kHidden>(ti, g, s);
+    default: return launch<kHead, 256>(g, s);
+  }
+}
+
+}  // namespace loss
+}  // namespace archead

@@ -93,3 +93,60 @@ def test_python_refuses_host_adapters():
     y, x = torch.zeros(2, 8), torch.zeros((2, 4), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         lib.adapters_add(y, x, x[None], x[None], torch.zeros(2, dtype=torch.int64))
+
+
+def _loss(L, gradient=False, **kw):
+    a = dict(x=P, ldx=64, w=P, ldw=64, y=P, t=ab.I64)
+    s = dict(M=2, V=100, d=64)
+    o = dict(dx=P, lddx=64, dw=P, lddw=64) if gradient else dict(loss=P, lse=P)
+    g = dict(lse=P, grad=P) if gradient else {}
+    e = dict(ws=P, wsb=1 << 30)
+    for v in (a, s, o, g, e):
+        v.update({k: kw[k] for k in kw if k in v})
+    f = L.archead_head_loss_grad if gradient else L.archead_head_loss
+    return f(*a.values(), *g.values(), *s.values(), *o.values(), *e.values(), None)
+
+
+BOTH = [
+    (dict(t=ab.F32), ab.E_INVALID_ARG), (dict(M=-1), ab.E_INVALID_ARG), (dict(V=0), ab.E_INVALID_ARG),
+    (dict(d=0), ab.E_INVALID_ARG), (dict(M=2 ** 20 + 1), ab.E_UNSUPPORTED), (dict(V=2 ** 22 + 1), ab.E_UNSUPPORTED),
+    (dict(d=16385, ldx=20000, ldw=20000, lddx=20000, lddw=20000), ab.E_UNSUPPORTED), (dict(ldx=63), ab.E_INVALID_ARG),
+    (dict(ldw=63), ab.E_INVALID_ARG), (dict(x=None), ab.E_INVALID_ARG), (dict(w=None), ab.E_INVALID_ARG),
+    (dict(y=None), ab.E_INVALID_ARG), (dict(x=P + 1), ab.E_MISALIGNED), (dict(w=P + 1), ab.E_MISALIGNED),
+    (dict(y=P + 4), ab.E_MISALIGNED), (dict(t=ab.I32, y=P + 2), ab.E_MISALIGNED), (dict(ws=None), ab.E_INVALID_ARG),
+    (dict(ws=P + 16), ab.E_MISALIGNED), (dict(wsb=1024), ab.E_WORKSPACE), (dict(lse=None), ab.E_INVALID_ARG),
+    (dict(lse=P + 2), ab.E_MISALIGNED),
+]
+
+
+@pytest.mark.parametrize("kw,status", BOTH + [
+    (dict(M=0), ab.OK), (dict(M=0, x=None, w=None, y=None, loss=None, ws=None), ab.OK), (dict(loss=None), ab.E_INVALID_ARG),
+    (dict(loss=P + 2), ab.E_MISALIGNED),
+])
+def test_head_loss_refusals(L, kw, status):
+    assert _loss(L, **kw) == status, L.archead_last_error()
+
+
+@pytest.mark.parametrize("kw,status", BOTH + [
+    (dict(M=0, dw=None), ab.OK), (dict(M=0, dx=None, dw=None), ab.OK), (dict(dx=None, dw=None), ab.E_INVALID_ARG),
+    (dict(grad=None), ab.E_INVALID_ARG), (dict(grad=P + 2), ab.E_MISALIGNED), (dict(lddx=63), ab.E_INVALID_ARG),
+    (dict(lddw=63), ab.E_INVALID_ARG), (dict(dx=P + 1), ab.E_MISALIGNED), (dict(dw=P + 1), ab.E_MISALIGNED),
+])
+def test_head_gradient_refusals(L, kw, status):
+    assert _loss(L, gradient=True, **kw) == status, L.archead_last_error()
+
+
+def test_head_loss_workspace_bytes(L):
+    f = L.archead_head_loss_workspace_bytes
+    assert f(0, 100, 64, P, 64, 0) == f(2, 0, 64, P, 64, 1) == f(2, 100, 16385, P, 20000, 0) == f(-1, 1, 1, P, 1, 0) == 0
+    assert f(2 ** 20 + 1, 1, 1, P, 1, 0) == f(1, 2 ** 22 + 1, 1, P, 1, 0) == 0
+    assert f(8, 100, 64, P + 2, 64, 0) > f(8, 100, 64, P, 64, 0)      # rows that have to be copied
+    assert f(4096, 151936, 4096, P, 4096, 0) < 4096 * 151936 // 4 and f(4096, 151936, 4096, P, 4096, 1) < 4096 * 151936 * 2 // 3
+
+
+def test_python_refuses_host_loss():
+    x = torch.zeros((2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        lib.head_loss(x, x, torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        lib.head_loss_grad(x, x, torch.zeros(2, dtype=torch.int64), torch.zeros(2), torch.zeros(2))
