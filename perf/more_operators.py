@@ -219,7 +219,7 @@ def run(state):
                 return lib.rms_norm_i8(s["x"], s["weight"], eps=_EPS, residual=s["residual"], offset=case["offset"],
                                        normed=case["normed"])
             out = lib.rms_norm(s["x"], s["weight"], eps=_EPS, residual=s["residual"], offset=case["offset"])
-            return out if isinstance(out, tuple) else (out,)
+            return out[::-1] if isinstance(out, tuple) else (out,)   # the sums first, as for 8 bits
         if op == "adapters":
             return lib.adapters_add(s["y"], s["x"], s["a"], s["b"], s["ids"], scales=s["scales"], ranks=s["ranks"])
         loss, lse = lib.head_loss(s["x"], s["w"], s["targets"])
