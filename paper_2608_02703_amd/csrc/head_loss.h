@@ -10,7 +10,7 @@ namespace loss {
 
 constexpr int kTileJ = 256;        // columns of a tile
 constexpr int kStageK = 64;        // k of a stage
-constexpr int kRowPad = 256;       // live tokens are padded with zero rows up to a multiple of this
+constexpr int kRowPad = 256;       // buffers hold this many tokens' rows or a multiple
 
 // The products, out[i, j] = sum_k: 
 //   kStats   i token, j vocabulary row, k of d: a tile's largest logit and sum of

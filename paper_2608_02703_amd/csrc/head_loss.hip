@@ -29,7 +29,7 @@ struct RowArgs {
   bool t64;
   int32_t* count;
   int32_t* pos;            // [M] place among the live tokens, or -1
-  int32_t* y;              // [Mp] by place, -1 for padding
+  int32_t* y;              // [Mp] by place
   float* lse_out;
   float* g_out;
   uint16_t* rows;          // [Mp][dp]
@@ -41,8 +41,8 @@ __device__ __forceinline__ int64_t target_of(const RowArgs& a, int64_t m) {
 }
 
 // The live tokens (those with a target in the vocabulary) back to back, in their
-// order, with zeros behind each row up to whole stages and behind the last token
-// up to a whole tile: tokens without a target cost no products, and nothing that
+// order, with zeros behind each row up to whole stages and behind the last token's
+// for sums over tokens: tokens without a target cost no products, and nothing that
 // their rows hold can reach a sum.  Each workgroup counts the live tokens before its own.
 __global__ __launch_bounds__(kRBlock) void k_ce_rows(RowArgs a) {
   __shared__ int32_t sums[2][kRBlock / 64], place[kRBlock];
@@ -94,26 +94,30 @@ __global__ __launch_bounds__(kRBlock) void k_ce_rows(RowArgs a) {
     }
     __syncthreads();
     const int here = int(std::min<int64_t>(kRBlock, end - m0));
-    // (a few rows: the whole workgroup on one after another; each thread its groups)
-    for (int i = 0; i < here; ++i) {
+    for (int i = wave; i < here; i += kRBlock / 64) {
       const int to = place[i];
       if (to < 0) continue;
       const uint8_t* const row = a.x + (m0 + i) * a.x_row;
-      for (int j = tid; j < groups; j += kRBlock) {
+      uint16_t* const out = a.rows + int64_t(to) * a.dp;
+      int j = lane;
+      for (; (j - lane + 256) * 8 <= a.d; j += 256) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = load_any<uint4>(row + (j + 64 * k) * 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(out + (j + 64 * k) * 8) = v[k];
+      }
+      for (; j < groups; j += 64) {
         Eight<ARCHEAD_BF16> e;
         e.load(row, int64_t(j) * 8, a.d, 0);
-        *reinterpret_cast<uint4*>(a.rows + int64_t(to) * a.dp + j * 8) = e.w[0];
+        *reinterpret_cast<uint4*>(out + j * 8) = e.w[0];
       }
     }
   }
-  for (int64_t r = all + blockIdx.x; r < (int64_t(all) + kRowPad - 1) / kRowPad * kRowPad; r += gridDim.x) {
+  if (!a.lse) return;   // (sums over tokens are the gradient's)
+  for (int64_t r = all + blockIdx.x; r < (int64_t(all) + kStageK - 1) / kStageK * kStageK; r += gridDim.x)
     for (int j = tid; j < groups; j += kRBlock)
       *reinterpret_cast<uint4*>(a.rows + r * a.dp + j * 8) = uint4{0, 0, 0, 0};
-    if (tid == 0) {
-      a.y[r] = -1;
-      if (a.lse) a.lse_out[r] = a.g_out[r] = 0.f;
-    }
-  }
 }
 
 // rows of the head padded with zeros to whole stages
@@ -269,7 +273,7 @@ hipError_t gather(const Plan& p, char* ws, const void* x, int64_t ldx, const voi
   RowArgs a{};
   a.x = static_cast<const uint8_t*>(x), a.target = targets, a.lse = lse, a.g = g;
   a.M = p.M, a.V = p.V, a.d = p.d, a.dp = p.dp, a.x_row = ldx * 2;
-  a.per_block = int(std::max<int64_t>(8, (p.M + 1023) / 1024));
+  a.per_block = int(std::max<int64_t>(4, (p.M + 1023) / 1024));
   a.t64 = tdt == ARCHEAD_I64;
   a.count = reinterpret_cast<int32_t*>(ws + p.count);
   a.pos = reinterpret_cast<int32_t*>(ws + p.pos);

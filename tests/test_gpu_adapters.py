@@ -65,7 +65,8 @@ def _check(i, out, before=None):
 TYPES = [("bf16", "bf16"), ("bf16", "f32"), ("bf16", "f16"), ("f16", "f16"), ("f16", "f32"), ("f16", "bf16")]
 SIZES = [(1, 64, 64, 16, 1), (1, 1, 1, 1, 1), (3, 7, 5, 3, 2), (16, 256, 512, 16, 16), (17, 100, 264, 8, 3),
          (64, 300, 128, 32, 70), (65, 513, 1000, 24, 4), (130, 1111, 333, 12, 5), (7, 4096, 4096, 64, 2),
-         (40, 250, 2048, 128, 3), (5, 130, 96, 200, 2), (33, 77, 640, 256, 3), (300, 96, 72, 50, 9)]
+         (40, 250, 2048, 128, 3), (5, 130, 96, 200, 2), (33, 77, 640, 256, 3), (300, 96, 72, 50, 9),
+         (600, 300, 128, 16, 200), (1, 64, 16384, 16, 1), (2, 70, 9001, 8, 2)]
 
 
 @pytest.mark.parametrize("dtype,y", TYPES)

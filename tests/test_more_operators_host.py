@@ -68,7 +68,7 @@ def _adapters(L, **kw):
     (dict(yt=ab.I8), ab.E_INVALID_ARG), (dict(xt=ab.F32), ab.E_INVALID_ARG), (dict(it=ab.F32), ab.E_INVALID_ARG),
     (dict(ad=False), ab.E_INVALID_ARG), (dict(M=-1), ab.E_INVALID_ARG), (dict(M=2 ** 31), ab.E_INVALID_ARG),
     (dict(N=2 ** 23 + 1, ldy=2 ** 24, ldo=2 ** 24), ab.E_INVALID_ARG), (dict(K=-1), ab.E_INVALID_ARG),
-    (dict(n=-1), ab.E_INVALID_ARG), (dict(n=2 ** 30), ab.E_INVALID_ARG), (dict(R=-1), ab.E_INVALID_ARG),
+    (dict(n=-1), ab.E_INVALID_ARG), (dict(n=2 ** 22), ab.E_INVALID_ARG), (dict(R=-1), ab.E_INVALID_ARG),
     (dict(R=257, b_row=300), ab.E_UNSUPPORTED), (dict(ldy=31), ab.E_INVALID_ARG), (dict(ldo=31), ab.E_INVALID_ARG),
     (dict(ldx=63), ab.E_INVALID_ARG), (dict(a_ad=-1), ab.E_INVALID_ARG), (dict(a_row=63), ab.E_INVALID_ARG),
     (dict(b_ad=2 ** 41), ab.E_INVALID_ARG), (dict(b_row=15), ab.E_INVALID_ARG), (dict(y=None), ab.E_INVALID_ARG),
