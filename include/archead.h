@@ -738,7 +738,7 @@ size_t archead_adapters_workspace_bytes(int64_t M, int64_t K, int64_t R, int64_t
  * Pointers are aligned to their element size; K and R that are multiples of 8
  * are fastest.  Results are reproducible.  `adapters` is read before the call
  * returns.  M = 0 or N = 0 is a no-op; n = 0, R = 0 or K = 0 adds nothing.
- * ARCHEAD_E_INVALID_ARG for a null pointer, a size < 0, M >= 2^31, N > 2^23, K > 2^24,
+ * ARCHEAD_E_INVALID_ARG for a null pointer, a size < 0, M or N > 2^23, K > 2^24,
  * n >= 2^22, a leading dimension or row stride too small, a stride < 0 or above 2^40, or a
  * dtype not listed; ARCHEAD_E_UNSUPPORTED for R > 256; ARCHEAD_E_MISALIGNED;
  * ARCHEAD_E_WORKSPACE; ARCHEAD_E_HIP when a launch fails. */

@@ -9,10 +9,8 @@ namespace {
 using namespace archead::rows;
 
 constexpr int kUBlock = 256, kUWaves = kUBlock / 64;   // threads and waves of the outer products' workgroups
-constexpr int kDBlock = 512, kDWaves = kDBlock / 64;   // of the inner ones'
 constexpr int64_t kMaxRank = 256;
-constexpr int kMaxSplit = 4;             // parts of K over workgroups at most
-constexpr size_t kTileLds = 40 * 1024;   // of a workgroup's tokens in LDS
+constexpr int64_t kMaxM = int64_t(1) << 23;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -28,15 +26,14 @@ struct AdaptArgs {
   const float* scales;     // may be null
   const int32_t* ranks;    // may be null
   uint8_t* out;
-  float* t;                // [splits][M][rank16]
+  uint4* t;                // operands [block][tile][32 ranks][part][64 lanes]
+  float* back;             // fp16: powers of two [block][tile][32 ranks][16 tokens]
   uint8_t* table;          // Groups of the blocks
   int64_t M, N, K, n;
   int64_t y_row, x_row, a_ad, a_row, b_ad, b_row, o_row;   // bytes
-  int R, rank16;
-  int splits, k_split;     // parts of K, elements of each
+  int R, kcs;              // operands of 32 ranks
   int spread;              // workgroups that share a block's tiles
-  int n_wg;                // outputs of a token per workgroup
-  int tiles_most;          // tiles of a workgroup of the outer products at most
+  int per_block;           // tiles that a block may hold
   bool ids64, in_place;
 };
 
@@ -139,33 +136,37 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, const f32x4
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// t[m, j] = sum_k x[m, k] a[j, k] over one part of K, fp32.  A workgroup takes a tile
-// of up to 16 tokens of one adapter and RC x 16 ranks, its waves shares of the
-// part of K, whose sums meet in LDS.  Both operands come straight from memory (16
-// rows of 64 bytes a load), the ranks as the first, so a lane's results are four
-// neighbouring ones of a token.  Lanes past the tile's tokens or the adapter's ranks
-// repeat the first: their results are not stored, and no load hangs on a branch.
-template <int DT, int RC, int TOK>
-__global__ __launch_bounds__(kDBlock, 4) void k_adapt_down(AdaptArgs p) {
+// t[m, j] = scale sum_k x[m, k] a[j, k] in fp32, written as the second operands of
+// k_adapt_up's products.  A workgroup takes a tile of up to 16 tokens of one adapter
+// and RC x 16 ranks, its WAVES waves pieces of K in turn, whose sums meet in LDS.  Both
+// operands come straight from memory (16 rows, all of a 128-byte line with two loads of
+// 16 bytes a lane: the order of k does not matter as long as both have the same), the
+// ranks as the first.  Lanes past the tile's tokens or the adapter's ranks repeat the
+// first: their results are not used, and no load hangs on a branch.
+//
+// t goes through the matrix units in PARTS parts of the operands' type: two hold 17
+// bits of it in bf16 and 22 in fp16 (there after a power of two that brings a token's
+// largest of 32 ranks to 2^14, so that no part is below the normal numbers), three 25.
+template <int DT, int RC, int TOK, int PARTS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
+  constexpr int STEPS = RC == 4 ? 4 : 8, PIECE = 32 * STEPS, ROW = RC * 16 + 4;
   __shared__ Groups<TOK> g;
-  constexpr int STEPS = RC == 4 ? 4 : 8;
-  __shared__ f32x4 part[kDWaves][RC][64];
+  __shared__ f32x4 part[WAVES][RC][64];
+  __shared__ float ts[16 * ROW];
   const int64_t m0 = int64_t(blockIdx.x) * TOK;
   group_tokens(g, p, m0, !p.in_place);
   if (blockIdx.y == 0 && blockIdx.z == 0)   // for k_adapt_up
-    for (int i = threadIdx.x; i < int(sizeof(g) / 16); i += kDBlock)
+    for (int i = threadIdx.x; i < int(sizeof(g) / 16); i += 64 * WAVES)
       reinterpret_cast<uint4*>(p.table + blockIdx.x * sizeof(g))[i] = reinterpret_cast<const uint4*>(&g)[i];
   const int lane = threadIdx.x & 63, lr = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int split = int(blockIdx.y) % p.splits, j0 = int(blockIdx.y) / p.splits * 16 * RC;
-  // the waves take pieces of the part in turn (rows of a power of two would have them
-  // all ask for the same memory channels with shares one behind another), then 32 at a time of the rest
-  constexpr int PIECE = 32 * STEPS;
-  const int K = int(p.K), begin = split * p.k_split, end = min(K, begin + p.k_split);
-  const int pieces = (end - begin) / PIECE, rest = begin + pieces * PIECE;
+  const int j0 = int(blockIdx.y) * 16 * RC, K = int(p.K);
+  // pieces of K to the waves in turn (shares one behind another would have rows of a
+  // power of two all ask for the same memory channels), then 32 at a time of the rest
+  const int pieces = K / PIECE;
   for (int ti = int(blockIdx.z); ti < g.tiles; ti += p.spread) {
     const int64_t id = g.adapter[ti];
     const int rank = g.rank[ti];
-    if (j0 >= rank) continue;
+    if (id < 0 || (j0 >= rank && j0 % 32 == 0)) continue;   // (operands are of 32 ranks: the second half of one is written)
     const bool there = lr < g.len[ti];
     const int64_t m = m0 + g.token[g.first[ti] + (there ? lr : 0)];
     const uint8_t* const x = p.x + m * p.x_row;
@@ -176,11 +177,11 @@ __global__ __launch_bounds__(kDBlock, 4) void k_adapt_down(AdaptArgs p) {
       a[c] = p.a + id * p.a_ad + (j < rank ? j : 0) * p.a_row;
     }
     f32x4 acc[RC] = {};
-    for (int i = wave; i < pieces; i += kDWaves) {   // all loads of a piece, then its products
+    for (int i = wave; i < pieces; i += WAVES) {   // all loads of a piece, then its products
       uint4 xv[STEPS], av[STEPS][RC];
 #pragma unroll
       for (int j = 0; j < STEPS; ++j) {
-        const int at = 2 * (begin + i * PIECE + 32 * j + 8 * q);
+        const int at = 2 * (i * PIECE + 64 * (j / 2) + 16 * q + 8 * (j % 2));
         xv[j] = load_any<uint4>(x + at);
 #pragma unroll
         for (int c = 0; c < RC; ++c) av[j][c] = load_any<uint4>(a[c] + at);
@@ -191,8 +192,7 @@ __global__ __launch_bounds__(kDBlock, 4) void k_adapt_down(AdaptArgs p) {
 #pragma unroll
         for (int c = 0; c < RC; ++c) acc[c] = mma<DT>(av[j][c], xv[j], acc[c]);
     }
-    const int last = rest + 32 * wave;   // (a piece is at most eight times 32)
-    if (last < end) {                    // zeros past K
+    for (int last = pieces * PIECE + 32 * wave; last < K; last += 32 * WAVES) {   // zeros past K
       Eight<ARCHEAD_BF16> e;
       e.load(x, last + 8 * q, K, 0);
       const uint4 xv = e.w[0];
@@ -205,14 +205,64 @@ __global__ __launch_bounds__(kDBlock, 4) void k_adapt_down(AdaptArgs p) {
 #pragma unroll
     for (int c = 0; c < RC; ++c) part[wave][c][lane] = acc[c];
     __syncthreads();
+    const float scale = p.scales ? p.scales[id] : 1.f;
     if (wave < RC) {
       f32x4 sum = part[0][wave][lane];
 #pragma unroll
-      for (int w = 1; w < kDWaves; ++w) sum += part[w][wave][lane];
-      if (there && j0 + 16 * wave < rank)
-        *reinterpret_cast<f32x4*>(p.t + (int64_t(split) * p.M + m) * p.rank16 + j0 + 16 * wave + 4 * q) = sum;
+      for (int w = 1; w < WAVES; ++w) sum += part[w][wave][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = j0 + 16 * wave + 4 * q + i < rank ? sum[i] * scale : 0.f;
+      *reinterpret_cast<f32x4*>(&ts[lr * ROW + 16 * wave + 4 * q]) = sum;
     }
     __syncthreads();
+    // operands of 32 ranks (RC = 1: half of one), a lane eight ranks of a token
+    constexpr int LANES = RC == 1 ? 32 : RC * 32;
+    const int u = threadIdx.x, jl = u / 16 * 8, kc = (j0 + jl) / 32, ql = (j0 + jl) % 32 / 8;
+    if (u < LANES && kc < p.kcs) {
+      float v[8], top = 0, pre = 1;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = ts[(u & 15) * ROW + jl + i];
+        top = fmaxf(top, fabsf(v[i]));
+      }
+      if constexpr (DT == ARCHEAD_F16) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        int e = 15;
+        if (top > 0 && top < INFINITY) frexpf(top, &e);
+        e = max(-100, min(100, 15 - e));
+        pre = ldexpf(1.f, e);
+        if (ql == 0) p.back[((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * 16 + (u & 15)] = ldexpf(1.f, -e);
+      }
+      uint32_t w[PARTS][4] = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float rest = v[i] * pre;
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          uint16_t bits;
+          float now;
+          if constexpr (DT == ARCHEAD_BF16) {
+            const __bf16 h = __bf16(rest);
+            now = float(h);
+            __builtin_memcpy(&bits, &h, 2);
+          } else {
+            const _Float16 h = _Float16(rest);
+            now = float(h);
+            __builtin_memcpy(&bits, &h, 2);
+          }
+          w[k][i / 2] |= uint32_t(bits) << (16 * (i & 1));
+          rest = fabsf(now) < INFINITY ? rest - now : 0.f;   // (an infinity or NaN has no rest)
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) {
+        uint4* const to = p.t + (((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * PARTS + k) * 64 + ql * 16 + (u & 15);
+        *to = uint4{w[k][0], w[k][1], w[k][2], w[k][3]};
+        if (RC == 1 && j0 % 32 == 0 && p.R <= j0 + 16) to[32] = uint4{0, 0, 0, 0};   // (no other workgroup has that half)
+      }
+    }
+    // (part is written again behind the next tile's loads, and ts behind its meeting)
   }
 }
 
@@ -239,76 +289,68 @@ __device__ __forceinline__ uint4 load_row(const uint8_t* row, int j, int R) {
   }
 }
 
-// out[m, n] = y[m, n] + sum_j t[m, j] b[n, j], t = scale times the sum of its parts.
-// t goes through the matrix units in PARTS parts of the operands' type: two hold 17
-// bits of it in bf16 and 22 in fp16 (there after a power of two that brings a
-// token's largest to 2^14, so that no part is below the normal numbers), three 25.
-// The workgroup holds the parts of its tokens in LDS; a wave takes 64 outputs of
-// a tile at a time, the rows of b as the first operand in an order that leaves a lane
-// with eight neighbouring outputs of a token twice.
-//
-// The loads of the next tile are on their way while one is computed, so none of them
-// may hang on a branch: lanes past a tile's tokens, items past the last and ranks
-// past the adapter's repeat others, and are masked where they are used.  HOLD: b's
-// rows stay in registers over the tiles of one adapter; else every tile loads its
-// own.  Only the last outputs of a row that is no multiple of 64 go one by one.
-// Bound by y and out.
-template <int DT, int DY, int R32, int TOK, int PARTS, int BR, bool HOLD>
+// out[m, n] = y[m, n] + sum_j t[m, j] b[n, j].  A wave takes up to TILES tiles and 64
+// outputs, once: all of their y and b's rows are asked for at the start, and the many
+// waves of a CU keep the memory busy (waves that walked along n with the next outputs'
+// loads ahead took 164 to 218 us for 8192 tokens).  b's rows are the first operand in
+// an order that leaves a lane with 16 neighbouring outputs of a token: every load and
+// store of 16 bytes a lane reaches into all of the tokens' 128-byte lines.  No load hangs
+// on a branch: lanes past a tile's tokens and ranks past the adapter's repeat others,
+// and are masked where they are used.  The last outputs of a row that is no multiple of
+// 64 go one by one.  Bound by y and out.
+template <int DT, int DY, int R32, int TOK, int PARTS, int BR, int TILES>
 __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_adapt_up(AdaptArgs p) {
-  constexpr int YB = Eight<DY>::kBytes, ROW = R32 * 32 + 8;   // elements of a token's row in LDS
-  __shared__ Groups<TOK> g;
-  __shared__ float back[TOK];    // fp16: the power of two to take out again
-  extern __shared__ __align__(16) uint16_t adapt_t[];          // [PARTS][16 tiles_most][ROW]
-  const int64_t m0 = int64_t(blockIdx.x) * TOK;
-  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q = lane >> 4, wave = tid >> 6;
-  for (int i = tid; i < int(sizeof(g) / 16); i += kUBlock)
-    reinterpret_cast<uint4*>(&g)[i] = reinterpret_cast<const uint4*>(p.table + blockIdx.x * sizeof(g))[i];
-  __syncthreads();
-  const int z = int(blockIdx.z), tiles = g.tiles > z ? (g.tiles - z + p.spread - 1) / p.spread : 0;   // of this workgroup
-  if (tiles == 0) return;
-  auto adapter_of = [&](int u) { return __builtin_amdgcn_readfirstlane(g.adapter[z + u * p.spread]); };
-  auto token_of = [&](int u) {
-    const int ti = z + u * p.spread;
-    return m0 + g.token[g.first[ti] + (lr < g.len[ti] ? lr : 0)];
-  };
-  int b_row[4];   // this lane's rows of b, from an item's first one on
+  constexpr int YB = Eight<DY>::kBytes;
+  const int lane = threadIdx.x & 63, lr = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t m0 = int64_t(blockIdx.z) * TOK;
+  const Groups<TOK>& g = reinterpret_cast<const Groups<TOK>*>(p.table)[blockIdx.z];
+  const int64_t n0 = (int64_t(blockIdx.x) * kUWaves + wave) * 64;
+  const int tiles = g.tiles, t0 = int(blockIdx.y) * TILES;
+  if (n0 >= p.N || t0 >= tiles) return;
+  const bool whole = n0 + 64 <= p.N;
+  int64_t at[TILES];
+  int id[TILES];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) b_row[c] = 32 * (c >> 1) + 8 * (lr >> 2) + 4 * (c & 1) + (lr & 3);
-  // eight outputs of a lane, twice: y's and where they lie
-  struct Held {
-    Eight<DY> y[2];
-    uint4 b[HOLD ? 1 : 4][R32];
-  };
-  constexpr int BATCH = !HOLD ? 2 : R32 <= 2 && DY != ARCHEAD_F32 ? 4 : 2;
-  uint4 bh[4][R32];
-  Held held[BATCH];
-  auto fetch_y = [&](Held& h, int u, int64_t n0) {
-    const uint8_t* const y = p.y + token_of(u) * p.y_row;
+  for (int u = 0; u < TILES; ++u) {
+    const int ti = min(t0 + u, tiles - 1), len = t0 + u < tiles ? g.len[ti] : 0;
+    at[u] = m0 + g.token[g.first[ti] + (lr < len ? lr : 0)];
+    id[u] = g.adapter[ti];
+  }
+  Eight<DY> yv[TILES][2];
+  if (whole)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) h.y[i].load(y, n0 + 32 * i + 8 * q, INT64_MAX, 0);
-  };
-  auto fetch_b = [&](uint4 (&b)[4][R32], int u, int64_t n0) {
-    const int64_t id = max(adapter_of(u), 0);   // (a tile without one does not use them)
-    const uint8_t* const rows = p.b + id * p.b_ad;
+    for (int u = 0; u < TILES; ++u)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint8_t* const row = rows + std::min(n0 + b_row[c], p.N - 1) * p.b_row;
+      for (int i = 0; i < 2; ++i) yv[u][i].load(p.y + at[u] * p.y_row, n0 + 16 * q + 8 * i, INT64_MAX, 0);
+  uint4 bv[4][R32];
 #pragma unroll
-      for (int kc = 0; kc < R32; ++kc) b[c][kc] = load_row<BR>(row, 32 * kc + 8 * q, p.R);
+  for (int u = 0; u < TILES; ++u) {
+    if (t0 + u >= tiles) break;
+    const int ti = t0 + u, rank = g.rank[ti];
+    if (u == 0 || id[u] != id[u > 0 ? u - 1 : 0]) {
+      const uint8_t* const b = p.b + std::max(id[u], 0) * p.b_ad;   // (a tile without one does not use it)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint8_t* const row = b + std::min(n0 + 16 * (lr >> 2) + 4 * c + (lr & 3), p.N - 1) * p.b_row;
+#pragma unroll
+        for (int kc = 0; kc < R32; ++kc) bv[c][kc] = load_row<BR>(row, 32 * kc + 8 * q, p.R);
+      }
     }
-  };
-  auto products = [&](f32x4 (&acc)[4], uint4 (&b)[4][R32], int u) {
-    const int rank = __builtin_amdgcn_readfirstlane(g.rank[z + u * p.spread]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] = f32x4{0, 0, 0, 0};
-    if (rank == 0) return;
+    f32x4 sum[4] = {};
 #pragma unroll
     for (int kc = 0; kc < R32; ++kc) {
+      if (32 * kc >= rank) break;
+      f32x4 acc[4] = {};
+      const int64_t op = (int64_t(blockIdx.z) * p.per_block + ti) * p.kcs + kc;
+      uint4 tv[PARTS];
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) tv[k] = p.t[(op * PARTS + k) * 64 + lane];
       if (rank < 32 * kc + 32) {   // b past the adapter's rank is not looked at
         const int j = 32 * kc + 8 * q;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          uint4& w = b[c][kc];
+          uint4& w = bv[c][kc];
           uint32_t d[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) d[i] = j + 2 * i + 1 < rank ? d[i] : j + 2 * i < rank ? d[i] & 0xffffu : 0u;
@@ -316,165 +358,50 @@ __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_ad
         }
       }
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) {
-        const uint4 tv = *reinterpret_cast<const uint4*>(&adapt_t[((k * p.tiles_most + u) * 16 + lr) * ROW + 32 * kc + 8 * q]);
+      for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) acc[c] = mma<DT>(b[c][kc], tv, acc[c]);
+        for (int c = 0; c < 4; ++c) acc[c] = mma<DT>(bv[c][kc], tv[k], acc[c]);
+      if constexpr (DT == ARCHEAD_F16) {
+        const float by = p.back[op * 16 + lr];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] += acc[c] * by;
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] += acc[c];
       }
     }
-    if constexpr (DT == ARCHEAD_F16) {
-      const float by = back[16 * u + lr];
+    if (lr >= g.len[ti]) continue;
+    uint8_t* const out = p.out + at[u] * p.o_row;
+    if (whole) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] *= by;
-    }
-  };
-  auto is_there = [&](int u) { return lr < g.len[z + u * p.spread]; };
-  // (where a tile has no adapter, y + 0: the same but for the sign of a zero, so it is not formed)
-  auto finish = [&](const Held& h, uint4 (&b)[4][R32], int u, int64_t n0) {
-    f32x4 acc[4];
-    products(acc, b, u);
-    const bool some = adapter_of(u) >= 0;
-    uint8_t* const out = p.out + token_of(u) * p.o_row;
-    if (!is_there(u)) return;
+      for (int i = 0; i < 2; ++i) {
+        f32x8 v;   // (y itself where there is no adapter: y + 0 loses the sign of a zero)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      f32x8 v;
+        for (int e = 0; e < 8; ++e) {
+          const float was = yv[u][i].at(e);
+          v[e] = id[u] >= 0 ? was + sum[2 * i + e / 4][e % 4] : was;
+        }
+        uint8_t* const to = out + (n0 + 16 * q + 8 * i) * YB;
+        if constexpr (DY == ARCHEAD_F32) store_any(to, v);
+        else if constexpr (DY == ARCHEAD_BF16) store_any(to, __builtin_convertvector(v, bf16x8));
+        else store_any(to, __builtin_convertvector(v, f16x8));
+      }
+    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = some ? h.y[i].at(e) + acc[2 * i + e / 4][e % 4] : h.y[i].at(e);
-      uint8_t* const to = out + (n0 + 32 * i + 8 * q) * YB;
-      if constexpr (DY == ARCHEAD_F32) store_any(to, v);
-      else if constexpr (DY == ARCHEAD_BF16) store_any(to, __builtin_convertvector(v, bf16x8));
-      else store_any(to, __builtin_convertvector(v, f16x8));
-    }
-  };
-  auto finish_last = [&](int u, int64_t n0) {   // outputs up to N, one by one
-    f32x4 acc[4];
-    fetch_b(bh, u, n0);
-    products(acc, bh, u);
-    const bool some = adapter_of(u) >= 0;
-    const int64_t m = token_of(u);
-    if (!is_there(u)) return;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int64_t n = n0 + 32 * i + 8 * q + e;
+      for (int i = 0; i < 16; ++i) {
+        const int64_t n = n0 + 16 * q + i;
         if (n >= p.N) continue;
-        const float more = some ? acc[2 * i + e / 4][e % 4] : 0.f;
         auto go = [&](auto* type) {
           typedef std::remove_pointer_t<decltype(type)> T;
-          const T v = *reinterpret_cast<const T*>(p.y + m * p.y_row + n * YB);
-          *reinterpret_cast<T*>(p.out + m * p.o_row + n * YB) = some ? T(float(v) + more) : v;
+          const T was = reinterpret_cast<const T*>(p.y + at[u] * p.y_row)[n];
+          reinterpret_cast<T*>(out)[n] = id[u] >= 0 ? T(float(was) + sum[i / 4][i % 4]) : was;
         };
         if constexpr (DY == ARCHEAD_F32) go(static_cast<float*>(nullptr));
         else if constexpr (DY == ARCHEAD_BF16) go(static_cast<__bf16*>(nullptr));
         else go(static_cast<_Float16*>(nullptr));
       }
-  };
-
-  // t of this workgroup's tiles: 16 lanes a token
-  auto stage = [&]() {
-#pragma unroll 2
-  for (int u = 0; u < tiles; ++u) {
-    const int ti = z + u * p.spread, i = tid >> 4, id = max(g.adapter[ti], 0), rank = g.rank[ti];
-    const bool there = i < g.len[ti];
-    const int64_t m = m0 + g.token[g.first[ti] + (there ? i : 0)];
-    const float scale = p.scales ? p.scales[id] : 1.f;
-    float v[R32 * 2], top = 0;
-#pragma unroll
-    for (int c = 0; c < R32 * 2; ++c) {
-      const int j = lr + 16 * c;
-      const float* const from = p.t + m * p.rank16 + min(j, p.rank16 - 1);
-      float sum = from[0];
-#pragma unroll
-      for (int s = 1; s < kMaxSplit; ++s) {
-        const float more = from[int64_t(min(s, p.splits - 1)) * p.M * p.rank16];
-        sum += s < p.splits ? more : 0.f;
-      }
-      v[c] = j < rank ? sum * scale : 0.f;
-      top = fmaxf(top, fabsf(v[c]));
-    }
-    float pre = 1;
-    if constexpr (DT == ARCHEAD_F16) {
-#pragma unroll
-      for (int s = 1; s < 16; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-      int e = 15;
-      if (top > 0 && top < INFINITY) frexpf(top, &e);
-      e = max(-100, min(100, 15 - e));
-      pre = ldexpf(1.f, e);
-      if (lr == 0) back[16 * u + i] = ldexpf(1.f, -e);
-    }
-#pragma unroll
-    for (int c = 0; c < R32 * 2; ++c) {
-      float rest = v[c] * pre;
-#pragma unroll
-      for (int k = 0; k < PARTS; ++k) {
-        uint16_t bits;
-        float part;
-        if constexpr (DT == ARCHEAD_BF16) {
-          const __bf16 h = __bf16(rest);
-          part = float(h);
-          __builtin_memcpy(&bits, &h, 2);
-        } else {
-          const _Float16 h = _Float16(rest);
-          part = float(h);
-          __builtin_memcpy(&bits, &h, 2);
-        }
-        adapt_t[((k * p.tiles_most + u) * 16 + i) * ROW + lr + 16 * c] = bits;
-        rest = fabsf(part) < INFINITY ? rest - part : 0.f;   // (an infinity or NaN has no rest)
-      }
     }
   }
-  __syncthreads();
-  };
-
-  const int64_t n_begin = int64_t(blockIdx.y) * p.n_wg + 64 * wave, n_end = std::min(p.N, (int64_t(blockIdx.y) + 1) * p.n_wg);
-  const int64_t n_whole = std::min(n_end, p.N / 64 * 64);
-  constexpr int STEP = 64 * kUWaves;
-  const int chunks = n_begin < n_whole ? int((n_whole - n_begin + STEP - 1) / STEP) : 0;   // of 64 outputs, of this wave
-  if constexpr (HOLD) {
-    stage();
-    for (int c = 0; c < chunks; ++c) {
-      const int64_t n0 = n_begin + int64_t(c) * STEP;
-      for (int u = 0; u < tiles;) {
-        const int id = adapter_of(u);
-        int end = u + 1;
-        while (end < tiles && adapter_of(end) == id) ++end;
-        fetch_b(bh, u, n0);
-        for (; u < end; u += BATCH) {
-#pragma unroll
-          for (int i = 0; i < BATCH; ++i) fetch_y(held[i], min(u + i, end - 1), n0);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int i = 0; i < BATCH; ++i)
-            if (u + i < end) finish(held[i], bh, u + i, n0);
-        }
-        u = end;
-      }
-    }
-  } else {
-    const int items = chunks * tiles;
-    auto fetch = [&](Held& h, int i) {
-      const int at = min(i, items - 1), c = at / tiles, u = at - c * tiles;
-      fetch_y(h, u, n_begin + int64_t(c) * STEP);
-      fetch_b(h.b, u, n_begin + int64_t(c) * STEP);
-    };
-    auto end = [&](Held& h, int i) {
-      const int c = i / tiles, u = i - c * tiles;
-      finish(h, h.b, u, n_begin + int64_t(c) * STEP);
-    };
-    if (items > 0) fetch(held[0], 0);
-    stage();
-    for (int i = 0; i < items; i += 2) {
-      fetch(held[1], i + 1);
-      end(held[0], i);
-      fetch(held[0], i + 2);
-      if (i + 1 < items) end(held[1], i + 1);
-    }
-  }
-  const int64_t n_last = p.N / 64 * 64;   // (at most one wave of a block has it)
-  if (n_last < p.N && n_last >= n_begin && n_last < n_end && (n_last - n_begin) % STEP == 0)
-    for (int u = 0; u < tiles; ++u) finish_last(u, n_last);
 }
 
 // rows of y where there is nothing to add
@@ -485,71 +412,56 @@ __global__ __launch_bounds__(kUBlock) void k_adapt_copy(const uint8_t* y, int64_
     *reinterpret_cast<uint16_t*>(to + j) = *reinterpret_cast<const uint16_t*>(from + j);
 }
 
-// Sizes of a call's launches, from its sizes alone, so that its sums have one order.
+// Sizes of a call's launches.
 struct Shape {
   int tok;                 // tokens of a block
-  int64_t tiles, in_block; // of 16 tokens of one adapter, in all and in a block: about as many as there may be
-  int rc, groups;          // ranks of a workgroup in sixteens, groups of them
-  int splits;
+  int64_t blocks, in_block;   // tiles of 16 tokens of one adapter that a block may hold
+  int kcs;                 // operands of 32 ranks
 };
-Shape shape(int64_t M, int64_t K, int64_t R, int64_t n) {
+Shape shape(int64_t M, int64_t R, int64_t n) {
   Shape s{};
   s.tok = M <= 64 ? 64 : 256;
-  const int64_t blocks = (M + s.tok - 1) / s.tok, in = std::min<int64_t>(s.tok, M);
+  s.blocks = (M + s.tok - 1) / s.tok;
+  const int64_t in = std::min<int64_t>(s.tok, M);
   s.in_block = std::min(in, n + 1 + in / 16);
-  s.tiles = blocks * s.in_block;
-  const int r16 = int((R + 15) / 16);
-  s.rc = r16 >= 3 ? 4 : r16 == 2 ? 2 : 1;
-  while (s.rc > 1 && s.tiles * ((r16 + s.rc - 1) / s.rc) < 256) s.rc /= 2;
-  s.groups = (r16 + s.rc - 1) / s.rc;
-  s.splits = 1;
-  while (s.splits < kMaxSplit && s.tiles * s.groups * s.splits < 128 && K / s.splits >= 4096) s.splits *= 2;
+  s.kcs = int((R + 31) / 32);
   return s;
 }
+constexpr int parts_of(int x_dtype, int y_dtype) { return y_dtype == ARCHEAD_F32 && x_dtype == ARCHEAD_BF16 ? 3 : 2; }
 
-size_t table_bytes(int64_t M, const Shape& s) {
-  return (size_t((M + s.tok - 1) / s.tok) * (s.tok == 64 ? sizeof(Groups<64>) : sizeof(Groups<256>)) + 255) / 256 * 256;
+template <int DT, int TOK, int PARTS>
+hipError_t down(AdaptArgs p, const Shape& sh, hipStream_t s) {
+  // Four waves to a tile and 64 ranks where there is a tile for every CU, else eight (of few
+  // tiles the least ranks to a workgroup too: fp16's powers of two are of 32).
+  const int r16 = (p.R + 15) / 16;
+  const auto go = [&](auto k, int rc, int waves) {
+    p.spread = int(std::min<int64_t>(sh.in_block, std::max<int64_t>(1, 65536 / sh.blocks)));
+    return launch_kernel(k, dim3(unsigned(sh.blocks), unsigned((r16 + rc - 1) / rc), unsigned(p.spread)), dim3(64 * waves), 0, s, p);
+  };
+  if (r16 >= 3 && sh.blocks * sh.in_block * ((r16 + 3) / 4) >= 256) return go(k_adapt_down<DT, 4, TOK, PARTS, 4>, 4, 4);
+  if constexpr (DT == ARCHEAD_F16) return go(k_adapt_down<DT, 2, TOK, PARTS, 8>, 2, 8);
+  else return go(k_adapt_down<DT, 1, TOK, PARTS, 8>, 1, 8);
 }
 
-template <int DT, int TOK>
-hipError_t down(const AdaptArgs& p, int rc, dim3 grid, hipStream_t s) {
-  const auto go = [&](auto k) { return launch_kernel(k, grid, dim3(kDBlock), 0, s, p); };
-  return rc == 1 ? go(k_adapt_down<DT, 1, TOK>) : rc == 2 ? go(k_adapt_down<DT, 2, TOK>) : go(k_adapt_down<DT, 4, TOK>);
+template <int DT, int DY, int R32, int TOK, int BR, int TILES>
+hipError_t up(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
+  const dim3 grid(unsigned((p.N + 64 * kUWaves - 1) / (64 * kUWaves)), unsigned((sh.in_block + TILES - 1) / TILES), unsigned(sh.blocks));
+  return launch_kernel(k_adapt_up<DT, DY, R32, TOK, parts_of(DT, DY), BR, TILES>, grid, dim3(kUBlock), 0, s, p);
 }
-
-template <int DT, int DY, int R32, int TOK, int BR, bool HOLD>
-hipError_t up(AdaptArgs p, const Shape& sh, hipStream_t s) {
-  constexpr int PARTS = DY == ARCHEAD_F32 && DT == ARCHEAD_BF16 ? 3 : 2;
-  constexpr size_t TILE = size_t(PARTS) * 16 * (R32 * 32 + 8) * 2;
-  const int64_t blocks = (p.M + TOK - 1) / TOK;
-  // Up to eight tiles to a workgroup (they share b's rows where they are of one
-  // adapter), and as many outputs as leave about four workgroups to a CU (they share t).
-  const int64_t chunks = (p.N + 63) / 64, each = (sh.tiles * chunks + 4095) / 4096;
-  const int64_t per = each >= 32 ? 8 : each >= 8 ? 4 : each >= 2 ? 2 : 1;
-  p.spread = int((sh.in_block + per - 1) / per);
-  constexpr int64_t STEP = 64 * kUWaves;
-  const int64_t steps = (p.N + STEP - 1) / STEP, wide = std::max<int64_t>(1, std::min(steps, 1024 / (blocks * p.spread)));
-  p.n_wg = int(STEP * ((steps + wide - 1) / wide));
-  // (a block may hold a tile for each of its tokens, or, of few adapters, fewer)
-  const int64_t most = std::min<int64_t>(TOK, p.n + 1 + TOK / 16);
-  p.tiles_most = int((most + p.spread - 1) / p.spread);
-  while (TILE * p.tiles_most > kTileLds && p.tiles_most > 1) {
-    ++p.spread;
-    p.tiles_most = int((most + p.spread - 1) / p.spread);
-  }
-  const dim3 grid(static_cast<unsigned>(blocks), unsigned((p.N + p.n_wg - 1) / p.n_wg), unsigned(p.spread));
-  return launch_kernel(k_adapt_up<DT, DY, R32, TOK, PARTS, BR, HOLD>, grid, dim3(kUBlock), TILE * p.tiles_most, s, p);
+// Four tiles to a wave (fp32 outputs two) where most tiles of a block are neighbours of
+// one adapter, one where most are of their own.
+template <int DT, int DY, int R32, int TOK, int BR>
+hipError_t up_tiles(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
+  constexpr int MANY = R32 <= 2 && DY != ARCHEAD_F32 ? 4 : 2;
+  return p.M >= 32 * p.n ? up<DT, DY, R32, TOK, BR, MANY>(p, sh, s) : up<DT, DY, R32, TOK, BR, 1>(p, sh, s);
 }
-// Ranks up to 64: b held where an adapter has 16 tokens of a block or more; the widest always
-// (two tiles' rows would not fit the registers).
 template <int DT, int DY, int TOK, int BR>
 hipError_t up_rank(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
-  const bool hold = std::min<int64_t>(TOK, p.M) >= 16 * p.n;
-  if (p.R <= 32) return hold ? up<DT, DY, 1, TOK, BR, true>(p, sh, s) : up<DT, DY, 1, TOK, BR, false>(p, sh, s);
+  if (p.R <= 32) return up_tiles<DT, DY, 1, TOK, BR>(p, sh, s);
   if constexpr (BR == kShort) return hipErrorInvalidValue;   // (of fewer than eight ranks)
-  else if (p.R <= 64) return hold ? up<DT, DY, 2, TOK, BR, true>(p, sh, s) : up<DT, DY, 2, TOK, BR, false>(p, sh, s);
-  else if (p.R <= 128) return up<DT, DY, 4, TOK, BR, true>(p, sh, s);
-  else return up<DT, DY, 8, TOK, BR, true>(p, sh, s);
+  else if (p.R <= 64) return up_tiles<DT, DY, 2, TOK, BR>(p, sh, s);
+  else if (p.R <= 128) return up_tiles<DT, DY, 4, TOK, BR>(p, sh, s);
+  else return up_tiles<DT, DY, 8, TOK, BR>(p, sh, s);
 }
 template <int DT, int TOK, int BR>
 hipError_t up_type(const AdaptArgs& p, archead_dtype y, const Shape& sh, hipStream_t s) {
@@ -559,30 +471,33 @@ hipError_t up_type(const AdaptArgs& p, archead_dtype y, const Shape& sh, hipStre
 }
 
 template <int DT, int TOK>
-hipError_t launch_tok(AdaptArgs p, archead_dtype y, const Shape& sh, hipStream_t s) {
-  const int64_t blocks = (p.M + TOK - 1) / TOK;
-  p.k_split = int(((p.K + sh.splits - 1) / sh.splits + 255) / 256 * 256);
-  p.splits = int((p.K + p.k_split - 1) / p.k_split);
-  p.spread = int(std::max<int64_t>(1, std::min(sh.in_block, 4096 / (blocks * p.splits * sh.groups))));
-  const hipError_t e =
-      down<DT, TOK>(p, sh.rc, dim3(static_cast<unsigned>(blocks), unsigned(p.splits * sh.groups), unsigned(p.spread)), s);
+hipError_t launch_tok(const AdaptArgs& p, archead_dtype y, const Shape& sh, hipStream_t s) {
+  const hipError_t e = parts_of(DT, y) == 3 ? down<DT, TOK, 3>(p, sh, s) : down<DT, TOK, 2>(p, sh, s);
   if (e != hipSuccess) return e;
   return p.R % 8 == 0 ? up_type<DT, TOK, kEights>(p, y, sh, s)
          : p.R > 8    ? up_type<DT, TOK, kOver>(p, y, sh, s)
                       : up_type<DT, TOK, kShort>(p, y, sh, s);
 }
-template <int DT>
-hipError_t launch(const AdaptArgs& p, archead_dtype y, hipStream_t s) {
-  const Shape sh = shape(p.M, p.K, p.R, p.n);
-  return sh.tok == 64 ? launch_tok<DT, 64>(p, y, sh, s) : launch_tok<DT, 256>(p, y, sh, s);
+
+// What a call keeps in its workspace, offsets in bytes.
+struct Space {
+  size_t t, back, total;   // (the blocks' groups first)
+};
+Space space(const Shape& s) {
+  const size_t tiles = size_t(s.blocks) * s.in_block;
+  auto up256 = [](size_t v) { return (v + 255) / 256 * 256; };
+  Space w{};
+  w.t = up256(s.blocks * (s.tok == 64 ? sizeof(Groups<64>) : sizeof(Groups<256>)));
+  w.back = w.t + tiles * s.kcs * 3 * 1024;
+  w.total = w.back + up256(tiles * s.kcs * 64);
+  return w;
 }
 
 }  // namespace
 
 extern "C" size_t archead_adapters_workspace_bytes(int64_t M, int64_t K, int64_t R, int64_t n) {
-  if (M < 1 || K < 1 || R < 1 || n < 1 || M > INT32_MAX || K > (1 << 24) || R > kMaxRank) return 0;
-  const Shape s = shape(M, K, R, n);
-  return table_bytes(M, s) + (size_t(s.splits) * M * ((R + 15) / 16 * 16) * 4 + 255) / 256 * 256;
+  if (M < 1 || K < 1 || R < 1 || n < 1 || M > kMaxM || K > (1 << 24) || R > kMaxRank) return 0;
+  return space(shape(M, R, n)).total;
 }
 
 extern "C" archead_status archead_adapters_add(const void* y, archead_dtype y_dtype, int64_t ldy, const void* x,
@@ -595,7 +510,7 @@ extern "C" archead_status archead_adapters_add(const void* y, archead_dtype y_dt
   if (!float_dtype(y_dtype)) return fail(ARCHEAD_E_INVALID_ARG, "y_dtype must be F32, BF16 or F16");
   if (x_dtype != ARCHEAD_BF16 && x_dtype != ARCHEAD_F16) return fail(ARCHEAD_E_INVALID_ARG, "x_dtype must be BF16 or F16");
   if (ids_dtype != ARCHEAD_I32 && ids_dtype != ARCHEAD_I64) return fail(ARCHEAD_E_INVALID_ARG, "ids_dtype must be I32 or I64");
-  if (M < 0 || M > INT32_MAX || N < 0 || N > (1 << 23) || K < 0 || K > (1 << 24))
+  if (M < 0 || M > kMaxM || N < 0 || N > (1 << 23) || K < 0 || K > (1 << 24))
     return fail(ARCHEAD_E_INVALID_ARG, "M = %lld, N = %lld, K = %lld out of range", (long long)M, (long long)N, (long long)K);
   if (!ad) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
   if (ad->n < 0 || ad->n >= (1 << 22) || ad->R < 0) return fail(ARCHEAD_E_INVALID_ARG, "n or R out of range");
@@ -630,17 +545,23 @@ extern "C" archead_status archead_adapters_add(const void* y, archead_dtype y_dt
   p.scales = ad->scales;
   p.ranks = ad->ranks;
   p.out = static_cast<uint8_t*>(out);
-  p.table = static_cast<uint8_t*>(ws);
-  p.t = any ? reinterpret_cast<float*>(p.table + table_bytes(M, shape(M, K, ad->R, ad->n))) : nullptr;
   p.M = M, p.N = N, p.K = K, p.n = any ? ad->n : 0;
   p.y_row = ldy * yb, p.x_row = ldx * 2, p.o_row = ldo * yb;
   p.a_ad = ad->a_adapter * 2, p.a_row = ad->a_row * 2, p.b_ad = ad->b_adapter * 2, p.b_row = ad->b_row * 2;
-  p.R = int(ad->R), p.rank16 = int((ad->R + 15) / 16 * 16);
+  p.R = int(ad->R);
   p.ids64 = ids_dtype == ARCHEAD_I64, p.in_place = out == y;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (!any)
     return launch_status(launch_kernel(k_adapt_copy, dim3(unsigned(M)), dim3(kUBlock), 0, s, p.y, p.y_row, p.out, p.o_row, N * yb),
                          "adapters launch");
-  return launch_status(x_dtype == ARCHEAD_BF16 ? launch<ARCHEAD_BF16>(p, y_dtype, s) : launch<ARCHEAD_F16>(p, y_dtype, s),
+  const Shape sh = shape(M, ad->R, ad->n);
+  const Space w = space(sh);
+  p.kcs = sh.kcs, p.per_block = int(sh.in_block);
+  p.table = static_cast<uint8_t*>(ws);
+  p.t = reinterpret_cast<uint4*>(p.table + w.t);
+  p.back = reinterpret_cast<float*>(p.table + w.back);
+  const bool bf = x_dtype == ARCHEAD_BF16, few = sh.tok == 64;
+  return launch_status(bf ? (few ? launch_tok<ARCHEAD_BF16, 64>(p, y_dtype, sh, s) : launch_tok<ARCHEAD_BF16, 256>(p, y_dtype, sh, s))
+                          : (few ? launch_tok<ARCHEAD_F16, 64>(p, y_dtype, sh, s) : launch_tok<ARCHEAD_F16, 256>(p, y_dtype, sh, s)),
                        "adapters launch");
 }
