@@ -137,8 +137,8 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, const f32x4
 }
 
 // t[m, j] = scale sum_k x[m, k] a[j, k] in fp32, written as the second operands of
-// k_adapt_up's products.  A workgroup takes a tile of up to 16 tokens of one adapter
-// and RC x 16 ranks, its WAVES waves pieces of K in turn, whose sums meet in LDS.  Both
+// k_adapt_up's products.  A workgroup takes a tile of up to 16 tokens of one adapter (TT
+// neighbouring ones of it, which share the loads of a) and RC x 16 ranks, its WAVES waves pieces of K in turn, whose sums meet in LDS.  Both
 // operands come straight from memory (16 rows, all of a 128-byte line with two loads of
 // 16 bytes a lane: the order of k does not matter as long as both have the same), the
 // ranks as the first.  Lanes past the tile's tokens or the adapter's ranks repeat the
@@ -147,8 +147,8 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, const f32x4
 // t goes through the matrix units in PARTS parts of the operands' type: two hold 17
 // bits of it in bf16 and 22 in fp16 (there after a power of two that brings a token's
 // largest of 32 ranks to 2^14, so that no part is below the normal numbers), three 25.
-template <int DT, int RC, int TOK, int PARTS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
+template <int DT, int RC, int TOK, int PARTS, int WAVES, int TT>
+__global__ __launch_bounds__(64 * WAVES, TT == 1 ? 4 : 2) void k_adapt_down(AdaptArgs p) {
   constexpr int STEPS = RC == 4 ? 4 : 8, PIECE = 32 * STEPS, ROW = RC * 16 + 4;
   __shared__ Groups<TOK> g;
   __shared__ f32x4 part[WAVES][RC][64];
@@ -163,26 +163,33 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
   // pieces of K to the waves in turn (shares one behind another would have rows of a
   // power of two all ask for the same memory channels), then 32 at a time of the rest
   const int pieces = K / PIECE;
-  for (int ti = int(blockIdx.z); ti < g.tiles; ti += p.spread) {
-    const int64_t id = g.adapter[ti];
-    const int rank = g.rank[ti];
+  for (int t0 = int(blockIdx.z) * TT; t0 < g.tiles; t0 += p.spread * TT)
+  for (int t1 = t0, run; t1 < min(t0 + TT, g.tiles); t1 += run) {   // tiles of one adapter
+    const int64_t id = g.adapter[t1];
+    const int rank = g.rank[t1];
+    run = 1;
+    while (run < TT - (t1 - t0) && t1 + run < g.tiles && g.adapter[t1 + run] == id) ++run;
     if (id < 0 || (j0 >= rank && j0 % 32 == 0)) continue;   // (operands are of 32 ranks: the second half of one is written)
-    const bool there = lr < g.len[ti];
-    const int64_t m = m0 + g.token[g.first[ti] + (there ? lr : 0)];
-    const uint8_t* const x = p.x + m * p.x_row;
+    const uint8_t* x[TT];
+#pragma unroll
+    for (int u = 0; u < TT; ++u) {
+      const int ti = t1 + min(u, run - 1);
+      x[u] = p.x + (m0 + g.token[g.first[ti] + (lr < g.len[ti] ? lr : 0)]) * p.x_row;
+    }
     const uint8_t* a[RC];
 #pragma unroll
     for (int c = 0; c < RC; ++c) {
       const int j = j0 + 16 * c + lr;
       a[c] = p.a + id * p.a_ad + (j < rank ? j : 0) * p.a_row;
     }
-    f32x4 acc[RC] = {};
+    f32x4 acc[TT][RC] = {};
     for (int i = wave; i < pieces; i += WAVES) {   // all loads of a piece, then its products
-      uint4 xv[STEPS], av[STEPS][RC];
+      uint4 xv[STEPS][TT], av[STEPS][RC];
 #pragma unroll
       for (int j = 0; j < STEPS; ++j) {
         const int at = 2 * (i * PIECE + 64 * (j / 2) + 16 * q + 8 * (j % 2));
-        xv[j] = load_any<uint4>(x + at);
+#pragma unroll
+        for (int u = 0; u < TT; ++u) xv[j][u] = load_any<uint4>(x[u] + at);
 #pragma unroll
         for (int c = 0; c < RC; ++c) av[j][c] = load_any<uint4>(a[c] + at);
       }
@@ -190,22 +197,33 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
 #pragma unroll
       for (int j = 0; j < STEPS; ++j)
 #pragma unroll
-        for (int c = 0; c < RC; ++c) acc[c] = mma<DT>(av[j][c], xv[j], acc[c]);
+        for (int u = 0; u < TT; ++u)
+#pragma unroll
+          for (int c = 0; c < RC; ++c) acc[u][c] = mma<DT>(av[j][c], xv[j][u], acc[u][c]);
     }
     for (int last = pieces * PIECE + 32 * wave; last < K; last += 32 * WAVES) {   // zeros past K
       Eight<ARCHEAD_BF16> e;
-      e.load(x, last + 8 * q, K, 0);
-      const uint4 xv = e.w[0];
+      uint4 xv[TT];
+#pragma unroll
+      for (int u = 0; u < TT; ++u) {
+        e.load(x[u], last + 8 * q, K, 0);
+        xv[u] = e.w[0];
+      }
 #pragma unroll
       for (int c = 0; c < RC; ++c) {
         e.load(a[c], last + 8 * q, K, 0);
-        acc[c] = mma<DT>(e.w[0], xv, acc[c]);
+#pragma unroll
+        for (int u = 0; u < TT; ++u) acc[u][c] = mma<DT>(e.w[0], xv[u], acc[u][c]);
       }
     }
-#pragma unroll
-    for (int c = 0; c < RC; ++c) part[wave][c][lane] = acc[c];
-    __syncthreads();
     const float scale = p.scales ? p.scales[id] : 1.f;
+#pragma unroll
+    for (int u = 0; u < TT; ++u) {
+    if (u >= run) break;
+    const int ti = t1 + u;
+#pragma unroll
+    for (int c = 0; c < RC; ++c) part[wave][c][lane] = acc[u][c];
+    __syncthreads();
     if (wave < RC) {
       f32x4 sum = part[0][wave][lane];
 #pragma unroll
@@ -217,12 +235,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
     __syncthreads();
     // operands of 32 ranks (RC = 1: half of one), a lane eight ranks of a token
     constexpr int LANES = RC == 1 ? 32 : RC * 32;
-    const int u = threadIdx.x, jl = u / 16 * 8, kc = (j0 + jl) / 32, ql = (j0 + jl) % 32 / 8;
-    if (u < LANES && kc < p.kcs) {
+    const int w = threadIdx.x, jl = w / 16 * 8, kc = (j0 + jl) / 32, ql = (j0 + jl) % 32 / 8;
+    if (w < LANES && kc < p.kcs) {
       float v[8], top = 0, pre = 1;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[i] = ts[(u & 15) * ROW + jl + i];
+        v[i] = ts[(w & 15) * ROW + jl + i];
         top = fmaxf(top, fabsf(v[i]));
       }
       if constexpr (DT == ARCHEAD_F16) {
@@ -232,9 +250,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
         if (top > 0 && top < INFINITY) frexpf(top, &e);
         e = max(-100, min(100, 15 - e));
         pre = ldexpf(1.f, e);
-        if (ql == 0) p.back[((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * 16 + (u & 15)] = ldexpf(1.f, -e);
+        if (ql == 0) p.back[((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * 16 + (w & 15)] = ldexpf(1.f, -e);
       }
-      uint32_t w[PARTS][4] = {};
+      uint32_t bits4[PARTS][4] = {};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float rest = v[i] * pre;
@@ -251,18 +269,19 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
             now = float(h);
             __builtin_memcpy(&bits, &h, 2);
           }
-          w[k][i / 2] |= uint32_t(bits) << (16 * (i & 1));
+          bits4[k][i / 2] |= uint32_t(bits) << (16 * (i & 1));
           rest = fabsf(now) < INFINITY ? rest - now : 0.f;   // (an infinity or NaN has no rest)
         }
       }
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) {
-        uint4* const to = p.t + (((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * PARTS + k) * 64 + ql * 16 + (u & 15);
-        *to = uint4{w[k][0], w[k][1], w[k][2], w[k][3]};
+        uint4* const to = p.t + (((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * PARTS + k) * 64 + ql * 16 + (w & 15);
+        *to = uint4{bits4[k][0], bits4[k][1], bits4[k][2], bits4[k][3]};
         if (RC == 1 && j0 % 32 == 0 && p.R <= j0 + 16) to[32] = uint4{0, 0, 0, 0};   // (no other workgroup has that half)
       }
     }
-    // (part is written again behind the next tile's loads, and ts behind its meeting)
+    // (part is written again when all have read it, ts behind the next meeting)
+    }
   }
 }
 
@@ -293,8 +312,8 @@ __device__ __forceinline__ uint4 load_row(const uint8_t* row, int j, int R) {
 // outputs, once: all of their y and b's rows are asked for at the start, and the many
 // waves of a CU keep the memory busy (waves that walked along n with the next outputs'
 // loads ahead took 164 to 218 us for 8192 tokens).  b's rows are the first operand in
-// an order that leaves a lane with 16 neighbouring outputs of a token: every load and
-// store of 16 bytes a lane reaches into all of the tokens' 128-byte lines.  No load hangs
+// an order that leaves 16 bytes of a token to a lane and 64 to four; t comes from LDS
+// (from memory, each wave for itself: 37 us more).  No load hangs
 // on a branch: lanes past a tile's tokens and ranks past the adapter's repeat others,
 // and are masked where they are used.  The last outputs of a row that is no multiple of
 // 64 go one by one.  Bound by y and out.
@@ -305,10 +324,16 @@ __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_ad
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t m0 = int64_t(blockIdx.z) * TOK;
   const Groups<TOK>& g = reinterpret_cast<const Groups<TOK>*>(p.table)[blockIdx.z];
+  extern __shared__ __align__(16) uint4 adapt_t[];   // [TILES][kcs][PARTS][64]
   const int64_t n0 = (int64_t(blockIdx.x) * kUWaves + wave) * 64;
   const int tiles = g.tiles, t0 = int(blockIdx.y) * TILES;
-  if (n0 >= p.N || t0 >= tiles) return;
+  if (t0 >= tiles) return;
   const bool whole = n0 + 64 <= p.N;
+  // A lane's results of the four products: 16 c + 4 q .. + 3 for fp32 outputs, and for
+  // 16-bit ones eight neighbours of two, so that 16 bytes a lane are 64 of a token.
+  constexpr bool F32 = DY == ARCHEAD_F32;
+  auto b_row = [&](int c) { return F32 ? 16 * c + lr : 32 * (c >> 1) + 8 * (lr >> 2) + 4 * (c & 1) + (lr & 3); };
+  auto n_of = [&](int i) { return F32 ? 16 * (i / 4) + 4 * q + i % 4 : 32 * (i / 8) + 8 * q + i % 8; };
   int64_t at[TILES];
   int id[TILES];
 #pragma unroll
@@ -317,26 +342,33 @@ __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_ad
     at[u] = m0 + g.token[g.first[ti] + (lr < len ? lr : 0)];
     id[u] = g.adapter[ti];
   }
-  Eight<DY> yv[TILES][2];
+  constexpr int NY = F32 ? 4 : 2;   // 16 bytes a lane
+  uint4 yv[TILES][NY], bv[4][R32];
+  auto fetch_b = [&](int id) {
+    const uint8_t* const b = p.b + std::max(id, 0) * p.b_ad;   // (a tile without an adapter does not use it)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint8_t* const row = b + std::min(n0 + b_row(c), p.N - 1) * p.b_row;
+#pragma unroll
+      for (int kc = 0; kc < R32; ++kc) bv[c][kc] = load_row<BR>(row, 32 * kc + 8 * q, p.R);
+    }
+  };
+  const int n_t = std::min(TILES, tiles - t0) * p.kcs * PARTS * 64;
+  const uint4* const t = p.t + (int64_t(blockIdx.z) * p.per_block + t0) * p.kcs * PARTS * 64;
+  for (int i = threadIdx.x; i < n_t; i += kUBlock) adapt_t[i] = t[i];
   if (whole)
 #pragma unroll
     for (int u = 0; u < TILES; ++u)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) yv[u][i].load(p.y + at[u] * p.y_row, n0 + 16 * q + 8 * i, INT64_MAX, 0);
-  uint4 bv[4][R32];
+      for (int i = 0; i < NY; ++i) yv[u][i] = load_any<uint4>(p.y + at[u] * p.y_row + (n0 + n_of(i * (16 / NY))) * YB);
+  fetch_b(id[0]);
+  __syncthreads();
+  if (n0 >= p.N) return;
 #pragma unroll
   for (int u = 0; u < TILES; ++u) {
     if (t0 + u >= tiles) break;
     const int ti = t0 + u, rank = g.rank[ti];
-    if (u == 0 || id[u] != id[u > 0 ? u - 1 : 0]) {
-      const uint8_t* const b = p.b + std::max(id[u], 0) * p.b_ad;   // (a tile without one does not use it)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint8_t* const row = b + std::min(n0 + 16 * (lr >> 2) + 4 * c + (lr & 3), p.N - 1) * p.b_row;
-#pragma unroll
-        for (int kc = 0; kc < R32; ++kc) bv[c][kc] = load_row<BR>(row, 32 * kc + 8 * q, p.R);
-      }
-    }
+    if (u > 0 && id[u] != id[u > 0 ? u - 1 : 0]) fetch_b(id[u]);
     f32x4 sum[4] = {};
 #pragma unroll
     for (int kc = 0; kc < R32; ++kc) {
@@ -345,7 +377,7 @@ __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_ad
       const int64_t op = (int64_t(blockIdx.z) * p.per_block + ti) * p.kcs + kc;
       uint4 tv[PARTS];
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) tv[k] = p.t[(op * PARTS + k) * 64 + lane];
+      for (int k = 0; k < PARTS; ++k) tv[k] = adapt_t[((u * p.kcs + kc) * PARTS + k) * 64 + lane];
       if (rank < 32 * kc + 32) {   // b past the adapter's rank is not looked at
         const int j = 32 * kc + 8 * q;
 #pragma unroll
@@ -374,22 +406,26 @@ __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_ad
     uint8_t* const out = p.out + at[u] * p.o_row;
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        f32x8 v;   // (y itself where there is no adapter: y + 0 loses the sign of a zero)
+      for (int i = 0; i < NY; ++i) {
+        if (id[u] >= 0) {   // (else y itself: y + 0 loses the sign of a zero)
+          if constexpr (F32) {
+            yv[u][i] = __builtin_bit_cast(uint4, __builtin_bit_cast(f32x4, yv[u][i]) + sum[i]);
+          } else {
+            Eight<DY> was;
+            was.w[0] = yv[u][i];
+            f32x8 v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float was = yv[u][i].at(e);
-          v[e] = id[u] >= 0 ? was + sum[2 * i + e / 4][e % 4] : was;
+            for (int e = 0; e < 8; ++e) v[e] = was.at(e) + sum[2 * i + e / 4][e % 4];
+            if constexpr (DY == ARCHEAD_BF16) yv[u][i] = __builtin_bit_cast(uint4, __builtin_convertvector(v, bf16x8));
+            else yv[u][i] = __builtin_bit_cast(uint4, __builtin_convertvector(v, f16x8));
+          }
         }
-        uint8_t* const to = out + (n0 + 16 * q + 8 * i) * YB;
-        if constexpr (DY == ARCHEAD_F32) store_any(to, v);
-        else if constexpr (DY == ARCHEAD_BF16) store_any(to, __builtin_convertvector(v, bf16x8));
-        else store_any(to, __builtin_convertvector(v, f16x8));
+        store_any(out + (n0 + n_of(i * (16 / NY))) * YB, yv[u][i]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int64_t n = n0 + 16 * q + i;
+        const int64_t n = n0 + n_of(i);
         if (n >= p.N) continue;
         auto go = [&](auto* type) {
           typedef std::remove_pointer_t<decltype(type)> T;
@@ -431,22 +467,25 @@ constexpr int parts_of(int x_dtype, int y_dtype) { return y_dtype == ARCHEAD_F32
 
 template <int DT, int TOK, int PARTS>
 hipError_t down(AdaptArgs p, const Shape& sh, hipStream_t s) {
-  // Four waves to a tile and 64 ranks where there is a tile for every CU, else eight (of few
-  // tiles the least ranks to a workgroup too: fp16's powers of two are of 32).
+  // Two tiles and 64 ranks to a workgroup where that leaves one for every CU (8192 x 4096, 64
+  // ranks of 8 adapters, one tile each: 63 us, 38 of them a's way through the L2s), else
+  // the least (fp16's powers of two are of 32).
   const int r16 = (p.R + 15) / 16;
-  const auto go = [&](auto k, int rc, int waves) {
-    p.spread = int(std::min<int64_t>(sh.in_block, std::max<int64_t>(1, 65536 / sh.blocks)));
-    return launch_kernel(k, dim3(unsigned(sh.blocks), unsigned((r16 + rc - 1) / rc), unsigned(p.spread)), dim3(64 * waves), 0, s, p);
+  const auto go = [&](auto k, int rc, int tt) {
+    p.spread = int((sh.in_block + tt - 1) / tt);
+    return launch_kernel(k, dim3(unsigned(sh.blocks), unsigned((r16 + rc - 1) / rc), unsigned(p.spread)), dim3(512), 0, s, p);
   };
-  if (r16 >= 3 && sh.blocks * sh.in_block * ((r16 + 3) / 4) >= 256) return go(k_adapt_down<DT, 4, TOK, PARTS, 4>, 4, 4);
-  if constexpr (DT == ARCHEAD_F16) return go(k_adapt_down<DT, 2, TOK, PARTS, 8>, 2, 8);
-  else return go(k_adapt_down<DT, 1, TOK, PARTS, 8>, 1, 8);
+  const int64_t full = (p.M + 15) / 16;   // tiles of tokens of one adapter each
+  if (r16 >= 3 && full / 2 * ((r16 + 3) / 4) >= 200) return go(k_adapt_down<DT, 4, TOK, PARTS, 8, 2>, 4, 2);
+  if constexpr (DT == ARCHEAD_F16) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 1);
+  else if (r16 >= 2 && sh.blocks * sh.in_block * r16 / 2 >= 200) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 1);
+  else return go(k_adapt_down<DT, 1, TOK, PARTS, 8, 1>, 1, 1);
 }
 
 template <int DT, int DY, int R32, int TOK, int BR, int TILES>
 hipError_t up(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
   const dim3 grid(unsigned((p.N + 64 * kUWaves - 1) / (64 * kUWaves)), unsigned((sh.in_block + TILES - 1) / TILES), unsigned(sh.blocks));
-  return launch_kernel(k_adapt_up<DT, DY, R32, TOK, parts_of(DT, DY), BR, TILES>, grid, dim3(kUBlock), 0, s, p);
+  return launch_kernel(k_adapt_up<DT, DY, R32, TOK, parts_of(DT, DY), BR, TILES>, grid, dim3(kUBlock), size_t(TILES) * sh.kcs * parts_of(DT, DY) * 1024, s, p);
 }
 // Four tiles to a wave (fp32 outputs two) where most tiles of a block are neighbours of
 // one adapter, one where most are of their own.
