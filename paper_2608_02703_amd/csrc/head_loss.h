@@ -29,6 +29,7 @@ struct TileArgs {
   int64_t depth;           // k (kHead: at most, the device's count says)
   const int32_t* count;    // live tokens
   int64_t v0;              // first vocabulary row of the piece
+  int64_t least_stages;    // kHidden: of the call's pieces
   // kStats
   float2* part;            // [token][n_part] (largest, sum)
   int64_t n_part, part0;   // tiles of the vocabulary; the piece's first one
@@ -40,11 +41,25 @@ struct TileArgs {
   uint16_t* out;           // kGrad: G [token][out_ld]; kHead: dw
   int64_t out_ld;
   // kHidden
-  float* sums;             // [split][row][sum_ld]
-  int64_t sum_ld, split_step;
-  int splits;              // parts of k
+  float* sums;             // [part of k][row][sum_ld], all in sum_rows rows
+  int64_t sum_ld, sum_rows;
   bool add;                // to what sums holds
 };
+
+// kHidden's parts of k: as many as bring its tiles to kTargetTiles and sums has rows
+// for, by the number of live tokens (the same in every piece, and where they are added up).
+constexpr int kTargetTiles = 256;
+constexpr int kMaxParts = 16;
+__host__ __device__ inline int64_t padded_rows(int64_t live) { return (live + kRowPad - 1) / kRowPad * kRowPad; }
+__host__ __device__ inline int splits_for(int64_t tiles, int64_t live, int64_t sum_rows, int64_t least_stages) {
+  if (live <= 0) return 1;
+  int64_t s = kTargetTiles / (tiles > 0 ? tiles : 1);
+  const int64_t fit = sum_rows / padded_rows(live);
+  s = s < fit ? s : fit;
+  s = s < kMaxParts ? s : kMaxParts;
+  s = s < least_stages ? s : least_stages;
+  return s > 1 ? int(s) : 1;
+}
 
 // tiles of ti x 256, ti = 64, 128 or 256 (kHead: 256)
 hipError_t launch_tiles(Op op, int ti, const TileArgs& g, hipStream_t s);

@@ -24,7 +24,7 @@ struct RowArgs {
   const void* target;
   const float* lse;        // by token, may be null
   const float* g;
-  int64_t M, V, d, dp, x_row;   // dp: d padded to whole stages; bytes of a row of x
+  int64_t M, V, d, dp, x_row, x_ld;   // dp: d padded to whole stages; bytes between rows of x, elements between those of `rows`
   int per_block;
   bool t64;
   int32_t* count;
@@ -32,7 +32,7 @@ struct RowArgs {
   int32_t* y;              // [Mp] by place
   float* lse_out;
   float* g_out;
-  uint16_t* rows;          // [Mp][dp]
+  uint16_t* rows;          // [Mp][x_ld]
 };
 
 __device__ __forceinline__ int64_t target_of(const RowArgs& a, int64_t m) {
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kRBlock) void k_ce_rows(RowArgs a) {
       const int to = place[i];
       if (to < 0) continue;
       const uint8_t* const row = a.x + (m0 + i) * a.x_row;
-      uint16_t* const out = a.rows + int64_t(to) * a.dp;
+      uint16_t* const out = a.rows + int64_t(to) * a.x_ld;
       int j = lane;
       for (; (j - lane + 256) * 8 <= a.d; j += 256) {
         uint4 v[4];
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kRBlock) void k_ce_rows(RowArgs a) {
   if (!a.lse) return;   // (sums over tokens are the gradient's)
   for (int64_t r = all + blockIdx.x; r < (int64_t(all) + kStageK - 1) / kStageK * kStageK; r += gridDim.x)
     for (int j = tid; j < groups; j += kRBlock)
-      *reinterpret_cast<uint4*>(a.rows + r * a.dp + j * 8) = uint4{0, 0, 0, 0};
+      *reinterpret_cast<uint4*>(a.rows + r * a.x_ld + j * 8) = uint4{0, 0, 0, 0};
 }
 
 // rows of the head padded with zeros to whole stages
@@ -164,10 +164,12 @@ __global__ __launch_bounds__(kRBlock) void k_ce_merge(const float2* part, int64_
 
 // The gradient of a token's hidden state from the parts of its sums, zeros for a
 // token without a target.
-__global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int splits, int64_t split_step, int64_t dp,
-                                                       const int32_t* pos, int64_t d, uint16_t* dx, int64_t ld) {
+__global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int64_t sum_rows, int64_t least_stages, int ti, int64_t dp,
+                                                       const int32_t* count, const int32_t* pos, int64_t d, uint16_t* dx, int64_t ld) {
   const int64_t m = blockIdx.x;
-  const int p = pos[m];
+  const int p = pos[m], live = *count;
+  const int splits = splits_for((live + ti - 1) / ti * ((d + kTileJ - 1) / kTileJ), live, sum_rows, least_stages);
+  const int64_t split_step = padded_rows(live) * dp;
   typedef float f32x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
   for (int64_t j = threadIdx.x * 8; j < d; j += kRBlock * 8) {
@@ -197,7 +199,9 @@ struct Plan {
   bool direct;             // the head's rows are read where they are
   int64_t piece;           // vocabulary rows at a time
   int64_t n_part;
-  int splits;              // of the hidden states' gradient
+  int64_t sum_rows;        // of the hidden states' gradient, in its parts
+  int64_t least_stages;    // of k in a piece
+  int64_t x_ld, g_ld;      // elements between rows of the tokens and of G
   size_t count, pos, y, tgt, part, lse, g, rows, copy, G, sums, total;
 };
 
@@ -216,8 +220,11 @@ Plan plan(int64_t M, int64_t V, int64_t d, bool direct, bool grad) {
   const int64_t i_tiles = (M + p.ti - 1) / p.ti;
   p.piece = std::min(p.piece, kTileJ * std::max<int64_t>(1, kMaxTiles / i_tiles));
   p.n_part = up(V, kTileJ) / kTileJ;
-  const int64_t tiles = i_tiles * (up(p.dp, kTileJ) / kTileJ);
-  p.splits = int(std::max<int64_t>(1, std::min<int64_t>(16, 256 / tiles)));
+  const int64_t tiles = i_tiles * (up(d, kTileJ) / kTileJ);
+  p.sum_rows = p.Mp * std::max<int64_t>(1, std::min<int64_t>(kMaxParts, kTargetTiles / tiles));
+  p.least_stages = ((V - 1) % p.piece + kStageK) / kStageK;
+  // rows of a power of two would all ask for the same memory channels at once
+  p.x_ld = p.dp + kStageK, p.g_ld = p.piece + kStageK;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -227,13 +234,13 @@ Plan plan(int64_t M, int64_t V, int64_t d, bool direct, bool grad) {
   p.count = take(4);
   p.pos = take(M * 4);
   p.y = take(p.Mp * 4);
-  p.rows = take(p.Mp * p.dp * 2);
+  p.rows = take(p.Mp * p.x_ld * 2);
   if (!direct) p.copy = take(p.piece * p.dp * 2);
   if (grad) {
     p.lse = take(p.Mp * 4);
     p.g = take(p.Mp * 4);
-    p.G = take(p.Mp * p.piece * 2);
-    p.sums = take(size_t(p.splits) * p.Mp * p.dp * 4);
+    p.G = take(p.Mp * p.g_ld * 2);
+    p.sums = take(p.sum_rows * p.dp * 4);
   } else {
     p.tgt = take(p.Mp * 4);
     p.part = take(p.Mp * p.n_part * 8);
@@ -272,7 +279,7 @@ hipError_t gather(const Plan& p, char* ws, const void* x, int64_t ldx, const voi
                   const float* lse, const float* g, hipStream_t s) {
   RowArgs a{};
   a.x = static_cast<const uint8_t*>(x), a.target = targets, a.lse = lse, a.g = g;
-  a.M = p.M, a.V = p.V, a.d = p.d, a.dp = p.dp, a.x_row = ldx * 2;
+  a.M = p.M, a.V = p.V, a.d = p.d, a.dp = p.dp, a.x_row = ldx * 2, a.x_ld = p.x_ld;
   a.per_block = int(std::max<int64_t>(4, (p.M + 1023) / 1024));
   a.t64 = tdt == ARCHEAD_I64;
   a.count = reinterpret_cast<int32_t*>(ws + p.count);
@@ -289,7 +296,7 @@ hipError_t gather(const Plan& p, char* ws, const void* x, int64_t ldx, const voi
 hipError_t piece_of(const Plan& p, char* ws, const void* w, int64_t ldw, int64_t v0, TileArgs& t, hipStream_t s) {
   t = TileArgs{};
   t.a = reinterpret_cast<const uint16_t*>(ws + p.rows);
-  t.a_ld = p.dp;
+  t.a_ld = p.x_ld;
   t.rows = p.M;
   t.cols = std::min(p.piece, p.V - v0);
   t.depth = p.dp;
@@ -366,30 +373,29 @@ extern "C" archead_status archead_head_loss_grad(const void* x, int64_t ldx, con
   hipError_t e = gather(p, base, x, ldx, targets, tgt_dtype, lse, grad, s);
   uint16_t* const G = reinterpret_cast<uint16_t*>(base + p.G);
   float* const sums = reinterpret_cast<float*>(base + p.sums);
-  const int64_t step = p.Mp * p.dp;
   for (int64_t v0 = 0; v0 < V && e == hipSuccess; v0 += p.piece) {
     TileArgs t;
     e = piece_of(p, base, w, ldw, v0, t, s);
     if (e != hipSuccess) break;
     TileArgs q = t;
     q.lse = reinterpret_cast<const float*>(base + p.lse), q.g = reinterpret_cast<const float*>(base + p.g);
-    q.out = G, q.out_ld = p.piece;
+    q.out = G, q.out_ld = p.g_ld;
     e = launch_tiles(kGrad, p.ti, q, s);
     if (dx && e == hipSuccess) {
       q = t;
-      q.a = G, q.a_ld = p.piece, q.cols = d, q.depth = t.cols;
-      q.sums = sums, q.sum_ld = p.dp, q.split_step = step, q.splits = p.splits, q.add = v0 > 0;
+      q.a = G, q.a_ld = p.g_ld, q.cols = d, q.depth = t.cols;
+      q.sums = sums, q.sum_ld = p.dp, q.sum_rows = p.sum_rows, q.least_stages = p.least_stages, q.add = v0 > 0;
       e = launch_tiles(kHidden, p.ti, q, s);
     }
     if (dw && e == hipSuccess) {
       q = t;
-      q.a = G, q.a_ld = p.piece, q.b = t.a, q.b_ld = t.a_ld, q.rows = t.cols, q.cols = d;
+      q.a = G, q.a_ld = p.g_ld, q.b = t.a, q.b_ld = t.a_ld, q.rows = t.cols, q.cols = d;
       q.out = static_cast<uint16_t*>(dw) + v0 * lddw, q.out_ld = lddw;
       e = launch_tiles(kHead, kTileJ, q, s);
     }
   }
   if (dx && e == hipSuccess)
-    e = launch_kernel(k_ce_hidden, dim3(unsigned(M)), dim3(kRBlock), 0, s, sums, p.splits, step, p.dp,
-                      reinterpret_cast<const int32_t*>(base + p.pos), d, static_cast<uint16_t*>(dx), lddx);
+    e = launch_kernel(k_ce_hidden, dim3(unsigned(M)), dim3(kRBlock), 0, s, sums, p.sum_rows, p.least_stages, p.ti, p.dp,
+                      reinterpret_cast<const int32_t*>(base + p.count), reinterpret_cast<const int32_t*>(base + p.pos), d, static_cast<uint16_t*>(dx), lddx);
   return launch_status(e, "head gradient launch");
 }

@@ -28,10 +28,10 @@ struct Geom {
   static constexpr int NS = 2;                                                  // stages in LDS
   static constexpr int ABYTES = TI * kStageK * 2, BBYTES = kTileJ * kStageK * 2, STAGE = ABYTES + BBYTES;
   static constexpr int LA = ABYTES / 1024 / NW, LB = BBYTES / 1024 / NW;        // loads of a wave and stage
-  static constexpr int OROW = kTileJ * 2 + 16;                                  // a row of 16-bit outputs in LDS, padded
-  static constexpr int RED = OP == kStats ? WJ * TI * 8 : 0;
-  static constexpr int BODY = std::max(NS * STAGE, OP == kGrad || OP == kHead ? TI * OROW : RED);
-  static constexpr int LDS = BODY;
+  // behind the stages: what the waves exchange (kStats), or their rows of 16-bit outputs: 16
+  // rows of their columns each, padded
+  static constexpr int OUT = NS * STAGE, OROW = NJ * 64 + 16;
+  static constexpr int LDS = OUT + (OP == kStats ? WJ * TI * 8 : OP == kHidden ? 0 : NW * 16 * OROW);
   static_assert(LDS <= 160 * 1024, "LDS budget");
   static_assert(!AT || TI == 256, "rows of k are 256 wide");
 };
@@ -159,13 +159,22 @@ struct Operand {
   static constexpr int kReads = BLOCKS * (T ? 2 : 1);
 };
 
+// LDS accesses of one wave stay in this order (the hardware keeps it; lanes read
+// what other lanes wrote, which the compiler does not see).
+__device__ __forceinline__ void wave_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+// All waves' LDS accesses are done; loads to LDS may go on.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <int OP, int TI>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_ce_tile(TileArgs g) {
   using G = Geom<OP, TI>;
   constexpr int NI = G::NI, NJ = G::NJ, NS = G::NS;
   extern __shared__ __align__(16) uint8_t ce_lds[];
   lds_u8* const L = (lds_u8*)ce_lds;
-  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wid / G::WJ, wj = wid % G::WJ;
   const int live = *g.count;
@@ -173,43 +182,61 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int64_t depth = OP == kHead ? (int64_t(live) + kStageK - 1) / kStageK * kStageK : g.depth;
 
   // workgroups go to the 8 XCDs in turn; each XCD takes a contiguous run of the
-  // order that walks groups of kRasterI tiles of i along j
-  const int i_tiles = int((rows + TI - 1) / TI), j_tiles = int((g.cols + kTileJ - 1) / kTileJ);
-  const int splits = OP == kHidden ? g.splits : 1;
-  const int n_all = i_tiles * j_tiles * splits, per_xcd = (n_all + 7) / 8;
-  const int lin = int(blockIdx.x & 7) * per_xcd + int(blockIdx.x >> 3);
-  if (int(blockIdx.x >> 3) >= per_xcd || lin >= n_all) return;
-  const int tile = lin % (i_tiles * j_tiles), split = lin / (i_tiles * j_tiles);
-  const int gsz = kRasterI * j_tiles, rg = tile / gsz, first = rg * kRasterI;
-  const int gi = min(i_tiles - first, kRasterI), within = tile - rg * gsz;
-  const int64_t i0 = int64_t(first + within % gi) * TI, j0 = int64_t(within / gi) * kTileJ;
-
+  // order that walks groups of kRasterI tiles of i along j, its workgroups in turn
+  const int i_tiles = int((rows + TI - 1) / TI), j_tiles = int((g.cols + kTileJ - 1) / kTileJ), ij = i_tiles * j_tiles;
   const int all_stages = int((depth + kStageK - 1) / kStageK);
-  const int s0 = int(int64_t(all_stages) * split / splits), s1 = int(int64_t(all_stages) * (split + 1) / splits);
-  const int stages = s1 - s0;
+  const int splits = OP == kHidden ? splits_for(ij, live, g.sum_rows, g.least_stages) : 1;
+  const int n_all = ij * splits, per_xcd = (n_all + 7) / 8, x0 = int(blockIdx.x & 7) * per_xcd;
+  const int end = min(per_xcd, n_all - x0), step = int(gridDim.x >> 3);
+  int cur = int(blockIdx.x >> 3);
+  if (cur >= end) return;
+  struct At {
+    int64_t i0, j0;
+    int split, s0, stages;
+  };
+  auto tile_at = [&](int t) {
+    const int lin = x0 + t, split = lin / ij, tile = lin - split * ij;
+    const int gsz = kRasterI * j_tiles, rg = tile / gsz, first = rg * kRasterI;
+    const int gi = min(i_tiles - first, kRasterI), within = tile - rg * gsz;
+    At r;
+    r.i0 = int64_t(first + within % gi) * TI;
+    r.j0 = int64_t(within / gi) * kTileJ;
+    r.split = split;
+    r.s0 = int(int64_t(all_stages) * split / splits);
+    r.stages = int(int64_t(all_stages) * (split + 1) / splits) - r.s0;
+    return r;
+  };
 
+  // ---- loads: the tile and stage they have come to
   Operand<G::AT, TI, G::LA, NI> a;
   Operand<G::BT, kTileJ, G::LB, NJ> b;
-  a.begin(g.a, g.a_ld, i0, OP == kHead ? (rows + 255) / 256 * 256 : rows, int64_t(all_stages) * kStageK, wid, lane);
-  b.begin(g.b, g.b_ld, j0, g.cols, OP == kHidden ? g.depth : depth, wid, lane);
   a.aim(wi * NI * 32, lane);
   b.aim(wj * NJ * 32, lane);
-  auto issue = [&](int s) {
-    lds_u8* const to = L + (s % NS) * G::STAGE;
-    const int64_t k0 = int64_t(s0 + s) * kStageK;
+  int l_tile = cur, l_stage = 0, l_slot = 0, l_s0 = 0, l_stages = 0;
+  auto begin = [&]() {
+    const At r = tile_at(l_tile);
+    l_s0 = r.s0, l_stages = r.stages, l_stage = 0;
+    a.begin(g.a, g.a_ld, r.i0, OP == kHead ? (rows + 255) / 256 * 256 : rows, int64_t(all_stages) * kStageK, wid, lane);
+    b.begin(g.b, g.b_ld, r.j0, g.cols, OP == kHidden ? g.depth : depth, wid, lane);
+  };
+  // the next stage of the sequence, if there is one
+  auto issue_next = [&]() {
+    if (l_tile >= end) return;
+    lds_u8* const to = L + l_slot * G::STAGE;
+    const int64_t k0 = int64_t(l_s0 + l_stage) * kStageK;
     a.issue(to, k0, wid, lane);
     b.issue(to + G::ABYTES, k0, wid, lane);
+    l_slot ^= 1;
+    if (++l_stage == l_stages) {
+      l_tile += step;
+      if (l_tile < end) begin();
+    }
   };
   b16x8 A[2][NI], B[2][NJ];
   f32x16 acc[NI][NJ];
-#pragma unroll
-  for (int i = 0; i < NI; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-  auto read = [&](int to, int s, int ks) {
-    const lds_u8* const from = L + (s % NS) * G::STAGE;
+  int slot = 0;   // of the stage being computed
+  auto read = [&](int to, int ks) {
+    const lds_u8* const from = L + slot * G::STAGE;
     a.read(A[to], from, ks);
     b.read(B[to], from + G::ABYTES, ks);
   };
@@ -221,40 +248,58 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(B[of][j], A[of][i], acc[i][j], 0, 0, 0);
   };
   constexpr int kReads = decltype(a)::kReads + decltype(b)::kReads, P = NI * NJ;
-  // A wave reads the operands of a K-step (16 k) during the step before.  Before the
-  // last step of a stage all its reads are done, so there the waves meet, once a
-  // stage: the next stage has landed, its first operands are read and the loads of
-  // the one after overwrite this one, all under the last step's products.
-  if (stages > 0) {
-    issue(0);
-    if (stages > 1) issue(1);
+  // A persistent workgroup per CU takes tiles in turn, their stages as one sequence: the
+  // loads run two stages ahead of the products, across tiles, so the next tile's first
+  // stages are on their way while one is written.  A wave reads the operands of a K-step
+  // (16 k) during the step before.  Before the last step of a stage all its reads are
+  // done, so there the waves meet, once a stage: the next stage has landed, its first
+  // operands are read and the loads of the one after overwrite this one, all under
+  // the last step's products.
+  if (all_stages > 0) {
+    begin();
+    issue_next();
+    issue_next();
     wait_loads_barrier<0>();
-    read(0, 0, 0);
-#pragma unroll 1
-    for (int s = 0; s < stages; ++s) {
-      __builtin_amdgcn_sched_barrier(0);
-      read(1, s, 1);
-      multiply(0);
-      spread<kReads, 0, P>();
-      read(0, s, 2);
-      multiply(1);
-      spread<kReads, 0, P>();
-      read(1, s, 3);
-      multiply(0);
-      spread<kReads, 0, P>();
-      wait_loads_barrier<0>();
-      __builtin_amdgcn_sched_barrier(0);
-      if (s + NS < stages) issue(s + NS);
-      if (s + 1 < stages) read(0, s + 1, 0);
-      multiply(1);
-    }
   }
+  auto stage = [&](auto more) {
+    __builtin_amdgcn_sched_barrier(0);
+    read(1, 1);
+    multiply(0);
+    spread<kReads, 0, P>();
+    read(0, 2);
+    multiply(1);
+    spread<kReads, 0, P>();
+    read(1, 3);
+    multiply(0);
+    spread<kReads, 0, P>();
+    wait_loads_barrier<0>();
+    __builtin_amdgcn_sched_barrier(0);
+    issue_next();
+    slot ^= 1;
+    if constexpr (decltype(more)::value) read(0, 0);
+    multiply(1);
+  };
+  for (; cur < end; cur += step) {
+  const At tile = tile_at(cur);
+  const int64_t i0 = tile.i0, j0 = tile.j0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+  if (tile.stages > 0) read(0, 0);
+#pragma unroll 1
+  for (int s = 1; s < tile.stages; ++s) stage(std::true_type{});
+  if (tile.stages > 0) stage(std::false_type{});   // (what is read ahead would not fit beside the outputs)
 
   // ---- outputs.  A lane's results: row i = lr of a block, columns 8 (r / 4) + 4 h + r % 4
   const int64_t jw = j0 + wj * NJ * 32;   // this wave's first column
+  int lane_here = lane;   // (its multiples are formed anew for each tile: kept over the stages they would not fit)
+  asm volatile("" : "+v"(lane_here));
+  const int lr = lane_here & 31, h = lane_here >> 5;
   if constexpr (OP == kStats) {
-    float2* const red = reinterpret_cast<float2*>(ce_lds);   // [WJ][TI]
-    __syncthreads();
+    float2* const red = reinterpret_cast<float2*>(ce_lds + G::OUT);   // [WJ][TI]
     const bool whole = j0 + kTileJ <= g.cols;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -268,34 +313,38 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
             if (jw + 32 * j + 8 * (r / 4) + 4 * h + r % 4 >= g.cols) acc[i][j][r] = -INFINITY;
       }
       float top = -INFINITY, sum = 0;
-      bool odd = false;   // a NaN among them
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          top = fmaxf(top, acc[i][j][r]);
-          odd |= acc[i][j][r] != acc[i][j][r];
-        }
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
       top = fmaxf(top, __shfl_xor(top, 32));
       if (top > -INFINITY) {
+        const float base = -top * kLog2e;   // (rounded once for all of a token: 2^-24 of top in the tile's log sum)
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - top) * kLog2e);
+          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, base));
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum = acc[i][j][r] != acc[i][j][r] ? NAN : sum;
       }
-      if (odd) sum = NAN;
       sum += __shfl_xor(sum, 32);
       if (h == 0) red[wj * TI + row] = float2{top, sum};
       const int64_t y = token < live ? g.target[token] - g.v0 - jw : -1;   // of this wave's columns
-      if (y >= 0 && y < NJ * 32 && (y >> 2 & 1) == h) {
+      const bool mine = y >= 0 && y < NJ * 32 && (int(y) >> 2 & 1) == h;
+      if (__ballot(mine) != 0) {
+        float hit = 0;
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (y == 32 * j + 8 * (r / 4) + 4 * h + r % 4) g.at_target[token] = acc[i][j][r];
+          for (int r = 0; r < 16; ++r) hit = (int(y) & ~4) == 32 * j + 8 * (r / 4) + r % 4 ? acc[i][j][r] : hit;
+        if (mine) g.at_target[token] = hit;
       }
+      __builtin_amdgcn_sched_barrier(0);   // (one token's values at a time in registers)
     }
-    __syncthreads();
+    meet();
     if (tid < TI && i0 + tid < live) {
       float top = -INFINITY, sum = 0;
 #pragma unroll
@@ -307,8 +356,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       }
       g.part[(i0 + tid) * g.n_part + g.part0 + j0 / kTileJ] = float2{top, sum};
     }
+    meet();   // (red has been read)
   } else if constexpr (OP == kHidden) {
-    float* const base = g.sums + split * g.split_step;
+    float* const base = g.sums + tile.split * padded_rows(live) * g.sum_ld;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       float* const row = base + (i0 + wi * NI * 32 + 32 * i + lr) * g.sum_ld;   // (rows are padded to whole tiles)
@@ -325,67 +375,88 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
     }
   } else {
-    // 16-bit rows through LDS, so that 32 lanes store what lies together
-    __syncthreads();
+    // 16-bit rows: each wave turns 16 at a time through its own part of the LDS, so
+    // that neighbouring lanes store what lies together
+    constexpr int LPR = NJ * 4;   // lanes to a row
+    uint8_t* const buf = ce_lds + G::OUT + wid * 16 * G::OROW;
     const int64_t cols = g.cols;
+    const bool whole = j0 + kTileJ <= cols;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int row = wi * NI * 32 + 32 * i + lr;
-      const int64_t token = i0 + row;
+      const int64_t row0 = i0 + wi * NI * 32 + 32 * i, token = row0 + lr;
       float lse = 0, gr = 0;
-      int64_t y = -1;
+      int y = -1;
       if constexpr (OP == kGrad) {
         if (token < live) {
           lse = g.lse[token];
           gr = g.g[token];
-          y = g.target[token] - g.v0 - jw;
+          const int64_t at = g.target[token] - g.v0 - jw;
+          y = at >= 0 && at < NJ * 32 ? int(at) : -1;
         }
       }
+      b16x4 out[NJ][4];
+      const float base = -lse * kLog2e;
+      const bool some = token < live;
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
+        for (int k = 0; k < 4; ++k) {
           f32x4v v;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            v[e] = acc[i][j][r + e];
+            v[e] = acc[i][j][4 * k + e];
             if constexpr (OP == kGrad) {
-              const int c = 32 * j + 2 * r + 4 * h + e;
-              float p = __builtin_amdgcn_exp2f((v[e] - lse) * kLog2e);
+              const int c = 32 * j + 8 * k + 4 * h + e;
+              float p = __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, base));
               if (y == c) p -= 1.f;
-              v[e] = token < live && jw + c < cols ? p * gr : 0.f;
+              v[e] = some && (whole || jw + c < cols) ? p * gr : 0.f;
             }
           }
-          const b16x4 o = __builtin_convertvector(v, b16x4);
-          *reinterpret_cast<b16x4*>(ce_lds + row * G::OROW + (wj * NJ * 32 + 32 * j + 2 * r + 4 * h) * 2) = o;
+          out[j][k] = __builtin_convertvector(v, b16x4);
         }
-    }
-    __syncthreads();
-    for (int row = tid >> 5; row < TI; row += 16) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(ce_lds + row * G::OROW + 16 * (tid & 31));
-      const int64_t j = j0 + 8 * (tid & 31);
-      uint16_t* const p = g.out + (i0 + row) * g.out_ld + j;
-      if constexpr (OP == kGrad) {   // (G has whole tiles)
-        *reinterpret_cast<u32x4*>(p) = v;
-      } else if (i0 + row < rows && j < cols) {
-        if (j + 8 <= cols) {
-          store_any(p, v);
-        } else {
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (j + e < cols) p[e] = uint16_t(w[e / 2] >> (16 * (e & 1)));
+      for (int t = 0; t < 32; t += 16) {
+        if ((lr & 16) == t) {
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              *reinterpret_cast<b16x4*>(buf + (lr & 15) * G::OROW + (32 * j + 8 * k + 4 * h) * 2) = out[j][k];
         }
+        wave_order();
+#pragma unroll
+        for (int r = lane_here / LPR; r < 16; r += 64 / LPR) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(buf + r * G::OROW + 16 * (lane_here % LPR));
+          const int64_t row = row0 + t + r, j = jw + 8 * (lane_here % LPR);
+          uint16_t* const p = g.out + row * g.out_ld + j;
+          if constexpr (OP == kGrad) {   // (G has whole tiles)
+            *reinterpret_cast<u32x4*>(p) = v;
+          } else if (row < rows && j < cols) {
+            if (j + 8 <= cols) {
+              store_any(p, v);
+            } else {
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (j + e < cols) p[e] = uint16_t(w[e / 2] >> (16 * (e & 1)));
+            }
+          }
+        }
+        wave_order();
       }
+      __builtin_amdgcn_sched_barrier(0);   // (one row's values at a time in registers)
     }
+  }
   }
 }
 
 template <int OP, int TI>
 hipError_t launch(const TileArgs& g, hipStream_t s) {
   const int64_t i_tiles = (g.rows + TI - 1) / TI, j_tiles = (g.cols + kTileJ - 1) / kTileJ;
-  const int64_t n = i_tiles * j_tiles * (OP == kHidden ? g.splits : 1);
-  return launch_kernel_lds(k_ce_tile<OP, TI>, dim3(unsigned((n + 7) / 8 * 8)), dim3(512), Geom<OP, TI>::LDS, s, g);
+  // (of fewer tokens than there may be, more parts: as many tiles as there may be)
+  const int64_t n = OP == kHidden ? kTargetTiles : i_tiles * j_tiles;
+  const int64_t per_xcd = std::max((n + 7) / 8, OP == kHidden ? (i_tiles * j_tiles + 7) / 8 : 0);
+  return launch_kernel_lds(k_ce_tile<OP, TI>, dim3(unsigned(8 * std::min<int64_t>(per_xcd, 32))), dim3(512), Geom<OP, TI>::LDS, s, g);
 }
 
 template <int OP>
