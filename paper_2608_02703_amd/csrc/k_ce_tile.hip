@@ -66,10 +66,10 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, lds_u8* to, u
 // by its place among four: the four rows of a read then lie in different banks.
 template <bool T, int ROWS, int LOADS, int BLOCKS>
 struct Operand {
-  const uint16_t* base;
-  int64_t ld, krows;       // krows (T): rows there are
-  int cols;                // T: columns there are, from the tile's first on
-  int bytes;               // T false: from base to the end of the last row
+  const uint16_t* next;    // the next stage's first element
+  int64_t ld, left;        // T: rows of k from there on
+  int there;               // rows of the tile, or T: columns
+  int bytes;               // that a whole stage reaches over
   uint32_t off[LOADS];
   uint32_t at[4];          // of a lane's reads
 
@@ -84,48 +84,50 @@ struct Operand {
       u = (o % 128 / 16) ^ swz_x(r);
     }
   }
-  // T false: `first` row of `all`; T true: `first` column of `all`, krows rows of k
-  __device__ __forceinline__ void begin(const uint16_t* p, int64_t ld_, int64_t first, int64_t all, int64_t k, int wid, int lane) {
+  // T false: `first` row of `all`; T true: `first` column of `all`, krows rows of k there are;
+  // and the stage that it begins with
+  __device__ __forceinline__ void begin(const uint16_t* p, int64_t ld_, int64_t first, int64_t all, int64_t krows, int stage, int wid,
+                                        int lane) {
+    constexpr int most = T ? kTileJ : ROWS;
     ld = ld_;
+    there = int(all - first < most ? all - first : most);
+    const int64_t k0 = int64_t(stage) * kStageK;
     if constexpr (T) {
-      base = p + first;
-      krows = k;
-      cols = int(all - first < kTileJ ? all - first : kTileJ);
+      next = p + k0 * ld + first;
+      left = krows - k0;
+      bytes = int(((kStageK - 1) * ld + ((there + 7) & ~7)) * 2);
     } else {
-      base = p + first * ld;
-      const int there = int(all - first < ROWS ? all - first : ROWS);
-      bytes = int(((there - 1) * ld + k) * 2);
-      cols = there;
+      next = p + first * ld + k0;
+      bytes = int(((there - 1) * ld + kStageK) * 2);
     }
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       int r, u;
       place(i, wid, lane, r, u);
-      off[i] = T ? uint32_t(r * ld * 2) + 2 * min(8 * u, (cols - 1) & ~7) : uint32_t(min(r, cols - 1) * ld * 2) + 16 * u;
+      off[i] = T ? uint32_t(r * ld * 2) + 2 * min(8 * u, (there - 1) & ~7) : uint32_t(min(r, there - 1) * ld * 2) + 16 * u;
     }
   }
-  __device__ __forceinline__ void issue(lds_u8* to, int64_t k0, int wid, int lane) {
-    if constexpr (T) {
-      const int left = int(krows - k0 < kStageK ? krows - k0 : kStageK);
-      const auto r64 = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + k0 * ld), 0,
-                                                         int(((left - 1) * ld + ((cols + 7) & ~7)) * 2), kBufferWord3);
-      if (left == kStageK) {
+  // a stage whose k are all there
+  __device__ __forceinline__ void issue_whole(lds_u8* to, int wid) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(next), 0, bytes, kBufferWord3);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          load_lds(r64, to + (wid * LOADS + i) * 1024, off[i], 0);
-      } else {   // rows past the last repeat it (the other operand has zeros there)
+    for (int i = 0; i < LOADS; ++i) load_lds(rsrc, to + (wid * LOADS + i) * 1024, off[i], 0);
+    next += T ? kStageK * ld : kStageK;
+    if constexpr (T) left -= kStageK;
+  }
+  __device__ __forceinline__ void issue(lds_u8* to, int wid, int lane) {
+    if (!T || left >= kStageK) {
+      issue_whole(to, wid);
+      return;
+    }
+    // rows past the last repeat it (the other operand has zeros there)
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(next), 0, int(((left - 1) * ld + ((there + 7) & ~7)) * 2),
+                                                        kBufferWord3);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          int r, u;
-          place(i, wid, lane, r, u);
-          load_lds(r64, to + (wid * LOADS + i) * 1024, uint32_t(min(r, left - 1) * ld * 2) + 2 * min(8 * u, (cols - 1) & ~7), 0);
-        }
-      }
-    } else {
-      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, bytes, kBufferWord3);
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        load_lds(rsrc, to + (wid * LOADS + i) * 1024, off[i], int(k0 * 2));
+    for (int i = 0; i < LOADS; ++i) {
+      int r, u;
+      place(i, wid, lane, r, u);
+      load_lds(rsrc, to + (wid * LOADS + i) * 1024, uint32_t(min(r, int(left) - 1) * ld * 2) + 2 * min(8 * u, (there - 1) & ~7), 0);
     }
   }
   // this wave's reads begin at row (column) `first` of the tile
@@ -212,20 +214,27 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   Operand<G::BT, kTileJ, G::LB, NJ> b;
   a.aim(wi * NI * 32, lane);
   b.aim(wj * NJ * 32, lane);
-  int l_tile = cur, l_stage = 0, l_slot = 0, l_s0 = 0, l_stages = 0;
+  int l_tile = cur, l_stage = 0, l_slot = 0, l_stages = 0;
   auto begin = [&]() {
     const At r = tile_at(l_tile);
-    l_s0 = r.s0, l_stages = r.stages, l_stage = 0;
-    a.begin(g.a, g.a_ld, r.i0, OP == kHead ? (rows + 255) / 256 * 256 : rows, int64_t(all_stages) * kStageK, wid, lane);
-    b.begin(g.b, g.b_ld, r.j0, g.cols, OP == kHidden ? g.depth : depth, wid, lane);
+    l_stages = r.stages, l_stage = 0;
+    a.begin(g.a, g.a_ld, r.i0, OP == kHead ? (rows + 255) / 256 * 256 : rows, depth, r.s0, wid, lane);
+    b.begin(g.b, g.b_ld, r.j0, g.cols, depth, r.s0, wid, lane);
   };
-  // the next stage of the sequence, if there is one
+  // a stage that is not its tile's last
+  auto issue_whole = [&]() {
+    lds_u8* const to = L + l_slot * G::STAGE;
+    a.issue_whole(to, wid);
+    b.issue_whole(to + G::ABYTES, wid);
+    l_slot ^= 1;
+    ++l_stage;
+  };
+  // any next stage of the sequence, if there is one
   auto issue_next = [&]() {
     if (l_tile >= end) return;
     lds_u8* const to = L + l_slot * G::STAGE;
-    const int64_t k0 = int64_t(l_s0 + l_stage) * kStageK;
-    a.issue(to, k0, wid, lane);
-    b.issue(to + G::ABYTES, k0, wid, lane);
+    a.issue(to, wid, lane);
+    b.issue(to + G::ABYTES, wid, lane);
     l_slot ^= 1;
     if (++l_stage == l_stages) {
       l_tile += step;
@@ -261,7 +270,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     issue_next();
     wait_loads_barrier<0>();
   }
-  auto stage = [&](auto more) {
+  auto steps = [&]() {   // of a stage but its last
     __builtin_amdgcn_sched_barrier(0);
     read(1, 1);
     multiply(0);
@@ -274,10 +283,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     spread<kReads, 0, P>();
     wait_loads_barrier<0>();
     __builtin_amdgcn_sched_barrier(0);
-    issue_next();
     slot ^= 1;
-    if constexpr (decltype(more)::value) read(0, 0);
-    multiply(1);
   };
   for (; cur < end; cur += step) {
   const At tile = tile_at(cur);
@@ -289,9 +295,25 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
   if (tile.stages > 0) read(0, 0);
+  int s = 0;
+  // stages whose loads are of this tile and not its last: no branches, the loads among the
+  // products (behind a branch, before them: 4096 x 151936 x 4096 4.39 ms for G, 4.62
+  // and 4.90 for the gradients)
 #pragma unroll 1
-  for (int s = 1; s < tile.stages; ++s) stage(std::true_type{});
-  if (tile.stages > 0) stage(std::false_type{});   // (what is read ahead would not fit beside the outputs)
+  for (; s < tile.stages - NS - 1; ++s) {
+    steps();
+    issue_whole();
+    read(0, 0);
+    multiply(1);
+    spread<kReads, G::LA + G::LB, P>();
+  }
+#pragma unroll 1
+  for (; s < tile.stages; ++s) {
+    steps();
+    issue_next();
+    if (s + 1 < tile.stages) read(0, 0);   // (beside the outputs they would not fit)
+    multiply(1);
+  }
 
   // ---- outputs.  A lane's results: row i = lr of a block, columns 8 (r / 4) + 4 h + r % 4
   const int64_t jw = j0 + wj * NJ * 32;   // this wave's first column
