@@ -454,7 +454,7 @@ def _norm_call(x, weight, eps, residual, offset, total, out, codes, scales):
     if residual is not None:
         ldr = _matrix(residual, "residual", gpu, x.dtype, (M, d))
         if total is None:
-            total = torch.empty((M, d), dtype=x.dtype, device=x.device)
+            total = x.new_empty((M, d))
         else:
             ldt = _matrix(total, "total", gpu, x.dtype, (M, d))
     elif total is not None:
@@ -478,7 +478,7 @@ def rms_norm(x, weight, eps=1e-6, residual=None, offset=0.0, out=None, total=Non
     residual or x, out may be x."""
     import torch
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = x.new_empty(x.shape)
     total = _norm_call(x, weight, eps, residual, offset, total, out, None, None)
     return out if residual is None else (out, total)
 
@@ -490,10 +490,10 @@ def rms_norm_i8(x, weight, eps=1e-6, residual=None, offset=0.0, normed=False, co
     (archead_rms_norm)."""
     import torch
     if codes is None:
-        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+        codes = x.new_empty(x.shape, dtype=torch.int8)
     if scales is None:
-        scales = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if normed is True else None if normed is False else normed
+        scales = x.new_empty(x.shape[0], dtype=torch.float32)
+    out = x.new_empty(x.shape) if normed is True else None if normed is False else normed
     total = _norm_call(x, weight, eps, residual, offset, total, out, codes, scales)
     return (codes, scales) + (() if residual is None else (total,)) + (() if out is None else (out,))
 

@@ -471,15 +471,15 @@ hipError_t down(AdaptArgs p, const Shape& sh, hipStream_t s) {
   // ranks of 8 adapters, one tile each: 63 us, 38 of them a's way through the L2s), else
   // the least (fp16's powers of two are of 32).
   const int r16 = (p.R + 15) / 16;
-  const auto go = [&](auto k, int rc, int tt) {
+  const auto go = [&](auto k, int rc, int waves, int tt) {
     p.spread = int((sh.in_block + tt - 1) / tt);
-    return launch_kernel(k, dim3(unsigned(sh.blocks), unsigned((r16 + rc - 1) / rc), unsigned(p.spread)), dim3(512), 0, s, p);
+    return launch_kernel(k, dim3(unsigned(sh.blocks), unsigned((r16 + rc - 1) / rc), unsigned(p.spread)), dim3(64 * waves), 0, s, p);
   };
   const int64_t full = (p.M + 15) / 16;   // tiles of tokens of one adapter each
-  if (r16 >= 3 && full / 2 * ((r16 + 3) / 4) >= 200) return go(k_adapt_down<DT, 4, TOK, PARTS, 8, 2>, 4, 2);
-  if constexpr (DT == ARCHEAD_F16) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 1);
-  else if (r16 >= 2 && sh.blocks * sh.in_block * r16 / 2 >= 200) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 1);
-  else return go(k_adapt_down<DT, 1, TOK, PARTS, 8, 1>, 1, 1);
+  if (r16 >= 3 && full / 2 * ((r16 + 3) / 4) >= 200) return go(k_adapt_down<DT, 4, TOK, PARTS, 8, 2>, 4, 8, 2);
+  if constexpr (DT == ARCHEAD_F16) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 8, 1);
+  else if (r16 >= 2 && sh.blocks * sh.in_block * r16 / 2 >= 200) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 8, 1);
+  else return go(k_adapt_down<DT, 1, TOK, PARTS, 8, 1>, 1, 8, 1);
 }
 
 template <int DT, int DY, int R32, int TOK, int BR, int TILES>

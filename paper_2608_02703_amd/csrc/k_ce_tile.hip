@@ -201,7 +201,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int gsz = kRasterI * j_tiles, rg = tile / gsz, first = rg * kRasterI;
     const int gi = min(i_tiles - first, kRasterI), within = tile - rg * gsz;
     At r;
-    r.i0 = int64_t(first + within % gi) * TI;
+    // (32 tiles later, where a workgroup goes on, another i: the last one may be cheaper)
+    const int turn = 32 % gi == 0 ? tile / 32 : 0;
+    r.i0 = int64_t(first + (within + turn) % gi) * TI;
     r.j0 = int64_t(within / gi) * kTileJ;
     r.split = split;
     r.s0 = int(int64_t(all_stages) * split / splits);
@@ -294,8 +296,19 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-  if (tile.stages > 0) read(0, 0);
   int s = 0;
+  // A wave whose rows are all past the last loads and meets the others only: the other
+  // wave of its SIMD has the matrix unit to itself, so a tile of half as many rows takes half
+  // the time.
+  if (i0 + wi * NI * 32 >= rows) {
+#pragma unroll 1
+    for (; s < tile.stages; ++s) {
+      wait_loads_barrier<0>();
+      slot ^= 1;
+      issue_next();
+    }
+  }
+  if (s < tile.stages) read(0, 0);
   // stages whose loads are of this tile and not its last: no branches, the loads among the
   // products (behind a branch, before them: 4096 x 151936 x 4096 4.39 ms for G, 4.62
   // and 4.90 for the gradients)
