@@ -29,7 +29,7 @@ struct TileArgs {
   int64_t depth;           // k (kHead: at most, the device's count says)
   const int32_t* count;    // live tokens
   int64_t v0;              // first vocabulary row of the piece
-  int64_t least_stages;    // kHidden: of the call's pieces
+  int64_t first_stages;    // kHidden: of the call's first piece
   // kStats
   float2* part;            // [token][n_part] (largest, sum)
   int64_t n_part, part0;   // tiles of the vocabulary; the piece's first one
@@ -47,21 +47,22 @@ struct TileArgs {
 };
 
 // kHidden's parts of k: as many as bring its tiles to kTargetTiles and sums has rows
-// for, by the number of live tokens (the same in every piece, and where they are added up).
+// for, by the number of live tokens (the same where they are added up; a shorter piece may
+// add to the first of them only).
 constexpr int kTargetTiles = 256;
-constexpr int kMaxParts = 16;
+constexpr int kPartStages = 8;     // stages of a part at least
 __host__ __device__ inline int64_t padded_rows(int64_t live) { return (live + kRowPad - 1) / kRowPad * kRowPad; }
-__host__ __device__ inline int splits_for(int64_t tiles, int64_t live, int64_t sum_rows, int64_t least_stages) {
+__host__ __device__ inline int splits_for(int64_t tiles, int64_t live, int64_t sum_rows, int64_t first_stages) {
   if (live <= 0) return 1;
   int64_t s = kTargetTiles / (tiles > 0 ? tiles : 1);
   const int64_t fit = sum_rows / padded_rows(live);
   s = s < fit ? s : fit;
-  s = s < kMaxParts ? s : kMaxParts;
-  s = s < least_stages ? s : least_stages;
+  const int64_t parts = first_stages / kPartStages;
+  s = s < parts ? s : parts;
   return s > 1 ? int(s) : 1;
 }
 
-// tiles of ti x 256, ti = 64, 128 or 256 (kHead: 256)
+// tiles of ti x 256, ti = 64, 128 or 256 (kHead: 128 or 256)
 hipError_t launch_tiles(Op op, int ti, const TileArgs& g, hipStream_t s);
 
 }  // namespace loss

@@ -168,18 +168,36 @@ __global__ __launch_bounds__(kRBlock) void k_ce_merge(const float2* part, int64_
 
 // The gradient of a token's hidden state from the parts of its sums, zeros for a
 // token without a target.
-__global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int64_t sum_rows, int64_t least_stages, int ti, int64_t dp,
+__global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int64_t sum_rows, int64_t first_stages, int ti, int64_t dp,
                                                        const int32_t* count, const int32_t* pos, int64_t d, uint16_t* dx, int64_t ld) {
   const int64_t m = blockIdx.x;
   const int p = pos[m], live = *count;
-  const int splits = splits_for((live + ti - 1) / ti * ((d + kTileJ - 1) / kTileJ), live, sum_rows, least_stages);
+  const int splits = splits_for((live + ti - 1) / ti * ((d + kTileJ - 1) / kTileJ), live, sum_rows, first_stages);
   const int64_t split_step = padded_rows(live) * dp;
   typedef float f32x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-  for (int64_t j = threadIdx.x * 8; j < d; j += kRBlock * 8) {
+  // many parts: a quarter of them to each wave
+  __shared__ f32x8 met[kRBlock / 64][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool shared = splits >= 8;
+  for (int64_t j0 = shared ? 0 : 512 * wave; j0 < d; j0 += shared ? 512 : 512 * (kRBlock / 64)) {
+    const int64_t j = j0 + 8 * lane;
     f32x8 v = {};
-    if (p >= 0)
-      for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x8*>(sums + s * split_step + p * dp + j);
+    if (p >= 0 && j < d) {
+      const float* const from = sums + p * dp + j;
+#pragma unroll 4
+      for (int s = shared ? wave : 0; s < splits; s += shared ? kRBlock / 64 : 1)
+        v += *reinterpret_cast<const f32x8*>(from + s * split_step);
+    }
+    if (shared) {
+      met[wave][lane] = v;
+      __syncthreads();
+      if (wave == 0)
+        for (int w = 1; w < kRBlock / 64; ++w) v += met[w][lane];
+      __syncthreads();
+      if (wave != 0) continue;
+    }
+    if (j >= d) continue;
     const bf16x8 o = __builtin_convertvector(v, bf16x8);
     uint16_t* const to = dx + m * ld + j;
     if (j + 8 <= d) {
@@ -199,12 +217,12 @@ __global__ __launch_bounds__(kRBlock) void k_ce_zero(uint16_t* w, int64_t d, int
 // What a call keeps in its workspace (offsets in bytes, multiples of 256).
 struct Plan {
   int64_t M, V, d, dp, Mp;
-  int ti;                  // tokens of a tile
+  int ti, ti_x, ti_w;      // rows of the tiles of logits, of the hidden states' and of the head's gradient
   bool direct;             // the head's rows are read where they are
   int64_t piece;           // vocabulary rows at a time
   int64_t n_part;
   int64_t sum_rows;        // of the hidden states' gradient, in its parts
-  int64_t least_stages;    // of k in a piece
+  int64_t first_stages;    // of k in the first piece, the longest
   int64_t x_ld, g_ld;      // elements between rows of the tokens and of G
   size_t count, pos, y, tgt, part, lse, g, rows, copy, G, sums, total;
 };
@@ -213,20 +231,39 @@ bool is_direct(const void* w, int64_t d, int64_t ldw) {
   return d % kStageK == 0 && ldw % 8 == 0 && ldw <= kMaxLdw && aligned(w, 16);
 }
 
+// Rows of the tiles of `rows` x `cols` tiles of columns: those of the least time, in rounds of
+// 256 tiles of which one of 128 (64) rows takes 0.62 (0.49) of one of 256's (256 x 65536 x 4096: one,
+// two and four rounds 156, 194 and 306 us).
+int rows_of_tiles(int64_t rows, int64_t cols, int least) {
+  int best = 256;
+  double time = 0;
+  for (const int t : {256, 128, 64}) {
+    if (t < least) continue;
+    const int64_t tiles = (rows + t - 1) / t * cols;
+    const double now = double((tiles + 255) / 256) * (t == 256 ? 1.0 : t == 128 ? 0.62 : 0.49);
+    if (t == 256 || now < 0.9 * time) {   // (near ties: the taller, whose last tile may be half empty)
+      best = t;
+      time = now;
+    }
+  }
+  return best;
+}
+
 Plan plan(int64_t M, int64_t V, int64_t d, bool direct, bool grad) {
   Plan p{};
   p.M = M, p.V = V, p.d = d, p.dp = up(d, kStageK), p.Mp = up(M, kRowPad);
-  p.ti = M <= 64 ? 64 : M <= 128 ? 128 : 256;
   p.direct = direct;
   p.piece = up(V, kTileJ);
   if (!direct) p.piece = std::min(p.piece, std::max<int64_t>(kTileJ, kPieceBytes / (p.dp * 2) / kTileJ * kTileJ));
   if (grad) p.piece = std::min(p.piece, std::max<int64_t>(16 * kTileJ, kPieceBytes / (p.Mp * 2) / kTileJ * kTileJ));
-  const int64_t i_tiles = (M + p.ti - 1) / p.ti;
-  p.piece = std::min(p.piece, kTileJ * std::max<int64_t>(1, kMaxTiles / i_tiles));
+  p.piece = std::min(p.piece, kTileJ * std::max<int64_t>(1, kMaxTiles / ((M + 63) / 64)));
+  p.ti = rows_of_tiles(M, up(p.piece, kTileJ) / kTileJ, 64);
+  p.ti_x = rows_of_tiles(M, 1 << 20, 64);   // (its parts of k fill the CUs)
+  p.ti_w = rows_of_tiles(std::min(V, p.piece), up(d, kTileJ) / kTileJ, 128);
   p.n_part = up(V, kTileJ) / kTileJ;
-  const int64_t tiles = i_tiles * (up(d, kTileJ) / kTileJ);
-  p.sum_rows = p.Mp * std::max<int64_t>(1, std::min<int64_t>(kMaxParts, kTargetTiles / tiles));
-  p.least_stages = ((V - 1) % p.piece + kStageK) / kStageK;
+  const int64_t tiles = (M + p.ti_x - 1) / p.ti_x * (up(d, kTileJ) / kTileJ);
+  p.first_stages = (std::min(V, p.piece) + kStageK - 1) / kStageK;
+  p.sum_rows = p.Mp * std::max<int64_t>(1, std::min<int64_t>(p.first_stages / kPartStages, kTargetTiles / tiles));
   // rows of a power of two would all ask for the same memory channels at once
   p.x_ld = p.dp + kStageK, p.g_ld = p.piece + kStageK;
   size_t at = 0;
@@ -388,18 +425,18 @@ extern "C" archead_status archead_head_loss_grad(const void* x, int64_t ldx, con
     if (dx && e == hipSuccess) {
       q = t;
       q.a = G, q.a_ld = p.g_ld, q.cols = d, q.depth = t.cols;
-      q.sums = sums, q.sum_ld = p.dp, q.sum_rows = p.sum_rows, q.least_stages = p.least_stages, q.add = v0 > 0;
-      e = launch_tiles(kHidden, p.ti, q, s);
+      q.sums = sums, q.sum_ld = p.dp, q.sum_rows = p.sum_rows, q.first_stages = p.first_stages, q.add = v0 > 0;
+      e = launch_tiles(kHidden, p.ti_x, q, s);
     }
     if (dw && e == hipSuccess) {
       q = t;
       q.a = G, q.a_ld = p.g_ld, q.b = t.a, q.b_ld = t.a_ld, q.rows = t.cols, q.cols = d;
       q.out = static_cast<uint16_t*>(dw) + v0 * lddw, q.out_ld = lddw;
-      e = launch_tiles(kHead, kTileJ, q, s);
+      e = launch_tiles(kHead, p.ti_w, q, s);
     }
   }
   if (dx && e == hipSuccess)
-    e = launch_kernel(k_ce_hidden, dim3(unsigned(M)), dim3(kRBlock), 0, s, sums, p.sum_rows, p.least_stages, p.ti, p.dp,
+    e = launch_kernel(k_ce_hidden, dim3(unsigned(M)), dim3(kRBlock), 0, s, sums, p.sum_rows, p.first_stages, p.ti_x, p.dp,
                       reinterpret_cast<const int32_t*>(base + p.count), reinterpret_cast<const int32_t*>(base + p.pos), d, static_cast<uint16_t*>(dx), lddx);
   return launch_status(e, "head gradient launch");
 }

@@ -33,7 +33,7 @@ struct Geom {
   static constexpr int OUT = NS * STAGE, OROW = NJ * 64 + 16;
   static constexpr int LDS = OUT + (OP == kStats ? WJ * TI * 8 : OP == kHidden ? 0 : NW * 16 * OROW);
   static_assert(LDS <= 160 * 1024, "LDS budget");
-  static_assert(!AT || TI == 256, "rows of k are 256 wide");
+  static_assert(!AT || TI >= 128, "rows of k have four parts of 64 bytes to swizzle");
 };
 
 // After each of the first products of a K-step a share of its R LDS reads; of V
@@ -60,7 +60,7 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, lds_u8* to, u
 
 // One operand's way to LDS and into registers.  T false: rows of the operand, 64 k =
 // 128 bytes each, their 16-byte units swizzled so that eight rows' reads of one unit
-// fall on eight different bank groups.  T true: rows of k, 256 columns = 512 bytes
+// fall on eight different bank groups.  T true: rows of k, ROWS columns (128 at least)
 // each; a group of 16 lanes reads four rows of 16 columns and gets them transposed,
 // so a lane has four k of its column.  There the 64-byte parts of a row are swizzled
 // by its place among four: the four rows of a read then lie in different banks.
@@ -77,8 +77,8 @@ struct Operand {
   static __device__ __forceinline__ void place(int i, int wid, int lane, int& r, int& u) {
     const int o = (wid * LOADS + i) * 1024 + 16 * lane;
     if constexpr (T) {
-      r = o / 512;
-      u = (o % 512 / 16) ^ (4 * (r & 3));
+      r = o / (ROWS * 2);
+      u = (o % (ROWS * 2) / 16) ^ (4 * (r & 3));
     } else {
       r = o / 128;
       u = (o % 128 / 16) ^ swz_x(r);
@@ -88,9 +88,8 @@ struct Operand {
   // and the stage that it begins with
   __device__ __forceinline__ void begin(const uint16_t* p, int64_t ld_, int64_t first, int64_t all, int64_t krows, int stage, int wid,
                                         int lane) {
-    constexpr int most = T ? kTileJ : ROWS;
     ld = ld_;
-    there = int(all - first < most ? all - first : most);
+    there = int(all - first < ROWS ? all - first : ROWS);
     const int64_t k0 = int64_t(stage) * kStageK;
     if constexpr (T) {
       next = p + k0 * ld + first;
@@ -137,7 +136,7 @@ struct Operand {
     for (int i = 0; i < 4; ++i) {
       if constexpr (T) {   // of block i
         const int row = (lane >> 2) & 3, unit = (first + 32 * i) / 8 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        at[i] = (8 * h + row) * 512 + 16 * (unit ^ (4 * row)) + 8 * (lane & 1);
+        at[i] = (8 * h + row) * (ROWS * 2) + 16 * (unit ^ (4 * row)) + 8 * (lane & 1);
       } else {             // of K-step i
         at[i] = (first + lr) * 128 + 16 * ((2 * i + h) ^ swz_x(lr));
       }
@@ -149,7 +148,7 @@ struct Operand {
       if constexpr (T) {
         auto half = [&](int j) {
           return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(from + at[i] + (16 * ks + 4 * j) * 512));
+              (__attribute__((address_space(3))) s16x4*)(from + at[i] + (16 * ks + 4 * j) * (ROWS * 2)));
         };
         const s16x4 lo = half(0), hi = half(1);
         to[i] = __builtin_bit_cast(b16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -187,7 +186,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   // order that walks groups of kRasterI tiles of i along j, its workgroups in turn
   const int i_tiles = int((rows + TI - 1) / TI), j_tiles = int((g.cols + kTileJ - 1) / kTileJ), ij = i_tiles * j_tiles;
   const int all_stages = int((depth + kStageK - 1) / kStageK);
-  const int splits = OP == kHidden ? splits_for(ij, live, g.sum_rows, g.least_stages) : 1;
+  const int splits =
+      OP == kHidden ? min(splits_for(ij, live, g.sum_rows, g.first_stages), max(1, all_stages / kPartStages)) : 1;
   const int n_all = ij * splits, per_xcd = (n_all + 7) / 8, x0 = int(blockIdx.x & 7) * per_xcd;
   const int end = min(per_xcd, n_all - x0), step = int(gridDim.x >> 3);
   int cur = int(blockIdx.x >> 3);
@@ -509,7 +509,7 @@ hipError_t launch_tiles(Op op, int ti, const TileArgs& g, hipStream_t s) {
     case kStats: return launch_op<kStats>(ti, g, s);
     case kGrad: return launch_op<kGrad>(ti, g, s);
     case kHidden: return launch_op<kHidden>(ti, g, s);
-    default: return launch<kHead, 256>(g, s);
+    default: return ti == 256 ? launch<kHead, 256>(g, s) : launch<kHead, 128>(g, s);
   }
 }
 
