@@ -25,7 +25,7 @@ struct Geom {
   static constexpr bool AT = OP == kHead, BT = OP == kHidden || OP == kHead;   // operands whose rows are k
   static constexpr int WI = TI >= 128 ? 2 : 1, WJ = 8 / WI, NW = 8;             // waves along i, j
   static constexpr int NI = TI / WI / 32, NJ = kTileJ / WJ / 32;                // blocks of 32 x 32 of a wave
-  static constexpr int NS = 2;                                                  // stages in LDS
+  static constexpr int NS = TI == 64 ? 3 : 2;                                   // stages in LDS
   static constexpr int ABYTES = TI * kStageK * 2, BBYTES = kTileJ * kStageK * 2, STAGE = ABYTES + BBYTES;
   static constexpr int LA = ABYTES / 1024 / NW, LB = BBYTES / 1024 / NW;        // loads of a wave and stage
   // behind the stages: what the waves exchange (kStats), or their rows of 16-bit outputs: 16
@@ -57,6 +57,13 @@ __device__ __forceinline__ void spread() {
 __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, lds_u8* to, uint32_t voff, int soff) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, reinterpret_cast<__attribute__((address_space(3))) void*>(to), 16, voff, soff, 0, 0);
 }
+
+// A transposing read of LDS.  (Of its own function, its argument restrict: the read then
+// carries the alias information without which the compiler waits, before each such read,
+// for every load to LDS that is on its way: the gradients 4.7 and 5.0 ms instead of
+// 4.1 and 4.2.)
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ s16x4 read_tr(lds_s16x4* __restrict p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
 
 // One operand's way to LDS and into registers.  T false: rows of the operand, 64 k =
 // 128 bytes each, their 16-byte units swizzled so that eight rows' reads of one unit
@@ -146,11 +153,9 @@ struct Operand {
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
       if constexpr (T) {
-        auto half = [&](int j) {
-          return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(from + at[i] + (16 * ks + 4 * j) * (ROWS * 2)));
-        };
-        const s16x4 lo = half(0), hi = half(1);
+        const lds_u8* const p = from + at[i] + 16 * ks * (ROWS * 2);
+        const s16x4 lo = read_tr(reinterpret_cast<lds_s16x4*>(const_cast<lds_u8*>(p)));
+        const s16x4 hi = read_tr(reinterpret_cast<lds_s16x4*>(const_cast<lds_u8*>(p + 4 * (ROWS * 2))));
         to[i] = __builtin_bit_cast(b16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       } else {
         to[i] = lds_load<b16x8>(from + at[ks] + 32 * i * 128);
@@ -228,7 +233,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     lds_u8* const to = L + l_slot * G::STAGE;
     a.issue_whole(to, wid);
     b.issue_whole(to + G::ABYTES, wid);
-    l_slot ^= 1;
+    l_slot = l_slot + 1 == NS ? 0 : l_slot + 1;
     ++l_stage;
   };
   // any next stage of the sequence, if there is one
@@ -237,7 +242,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     lds_u8* const to = L + l_slot * G::STAGE;
     a.issue(to, wid, lane);
     b.issue(to + G::ABYTES, wid, lane);
-    l_slot ^= 1;
+    l_slot = l_slot + 1 == NS ? 0 : l_slot + 1;
     if (++l_stage == l_stages) {
       l_tile += step;
       if (l_tile < end) begin();
@@ -260,7 +265,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   };
   constexpr int kReads = decltype(a)::kReads + decltype(b)::kReads, P = NI * NJ;
   // A persistent workgroup per CU takes tiles in turn, their stages as one sequence: the
-  // loads run two stages ahead of the products, across tiles, so the next tile's first
+  // loads run NS stages ahead of the products, across tiles, so the next tile's first
   // stages are on their way while one is written.  A wave reads the operands of a K-step
   // (16 k) during the step before.  Before the last step of a stage all its reads are
   // done, so there the waves meet, once a stage: the next stage has landed, its first
@@ -268,11 +273,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   // the last step's products.
   if (all_stages > 0) {
     begin();
-    issue_next();
-    issue_next();
+#pragma unroll
+    for (int i = 0; i < NS; ++i) issue_next();
     wait_loads_barrier<0>();
   }
-  auto steps = [&]() {   // of a stage but its last
+  auto next_slot = [&]() { slot = slot + 1 == NS ? 0 : slot + 1; };
+  // The steps of a stage but its last, and the meeting: with the loads of all stages but the next
+  // one in flight where whole ones follow it, else with none.
+  auto steps = [&](auto whole) {
+    constexpr int AHEAD = decltype(whole)::value ? (NS - 2) * (G::LA + G::LB) : 0;
     __builtin_amdgcn_sched_barrier(0);
     read(1, 1);
     multiply(0);
@@ -283,9 +292,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     read(1, 3);
     multiply(0);
     spread<kReads, 0, P>();
-    wait_loads_barrier<0>();
+    wait_loads_barrier<AHEAD>();
     __builtin_amdgcn_sched_barrier(0);
-    slot ^= 1;
+    next_slot();
   };
   for (; cur < end; cur += step) {
   const At tile = tile_at(cur);
@@ -304,17 +313,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll 1
     for (; s < tile.stages; ++s) {
       wait_loads_barrier<0>();
-      slot ^= 1;
+      next_slot();
       issue_next();
     }
   }
   if (s < tile.stages) read(0, 0);
   // stages whose loads are of this tile and not its last: no branches, the loads among the
-  // products (behind a branch, before them: 4096 x 151936 x 4096 4.39 ms for G, 4.62
-  // and 4.90 for the gradients)
+  // products (behind a branch, before them: logits of 4096 x 151936 x 4096 3.83 ms, so 3.74)
 #pragma unroll 1
   for (; s < tile.stages - NS - 1; ++s) {
-    steps();
+    steps(std::true_type{});
     issue_whole();
     read(0, 0);
     multiply(1);
@@ -322,7 +330,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 #pragma unroll 1
   for (; s < tile.stages; ++s) {
-    steps();
+    steps(std::false_type{});
     issue_next();
     if (s + 1 < tile.stages) read(0, 0);   // (beside the outputs they would not fit)
     multiply(1);
