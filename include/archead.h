@@ -641,12 +641,12 @@ archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const float* a_sc
  *             scales device fp32 [M].  out or codes must be there.
  *   stream    hipStream_t (NULL = the default stream); asynchronous
  * Pointers are aligned to their element size, leading dimensions >= d; what
- * lies between rows is left as it was.  total may be x or residual, and out
- * may be x, with the same leading dimension (not both x); otherwise outputs share no
+ * lies between rows is left as it was.  total and out may each be x or residual, with
+ * its leading dimension, but not both the same; otherwise outputs share no
  * memory with inputs or each other.  Results are reproducible.  M = 0 is a
  * no-op.  ARCHEAD_E_INVALID_ARG for a null pointer, M < 0 or M >= 2^31, d < 1,
- * a leading dimension < d, an eps that is not positive and finite, an offset
- * that is not finite, or a dtype not listed; ARCHEAD_E_UNSUPPORTED for
+ * a leading dimension < d or in place another one, total == out, an eps that is not
+ * positive and finite, an offset that is not finite, or a dtype not listed; ARCHEAD_E_UNSUPPORTED for
  * d > 16384; ARCHEAD_E_MISALIGNED; ARCHEAD_E_HIP when the launch fails. */
 archead_status archead_rms_norm(const void* x, archead_dtype dtype, int64_t M, int64_t d, int64_t ldx,
                                 const void* residual, int64_t ldr, const void* weight,

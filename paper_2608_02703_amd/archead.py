@@ -474,8 +474,8 @@ def rms_norm(x, weight, eps=1e-6, residual=None, offset=0.0, out=None, total=Non
     """Root-mean-square norm of the rows of x (float32, bfloat16 or float16
     [M, d] on the GPU, d <= 16384), of x + residual where one is given, times
     offset + weight (archead_rms_norm).  Returns the normed rows, and with a
-    residual (normed rows, x + residual).  total (where the sum goes) may be
-    residual or x, out may be x."""
+    residual (normed rows, x + residual).  total (where the sum goes) and out may
+    each be residual or x, but not both the same."""
     import torch
     if out is None:
         out = x.new_empty(x.shape)

@@ -13,11 +13,10 @@ using namespace archead::loss;
 
 constexpr int64_t kMaxM = int64_t(1) << 20, kMaxV = int64_t(1) << 22, kMaxD = 16384;
 constexpr int64_t kMaxLdw = int64_t(1) << 20;           // a tile's rows stay within 31-bit offsets
-// Of G, and of a copy of the head's rows: about 1024 tiles of G, so that a last round of
-// 256 that is not full costs little, and two pieces stay in the last cache (4096 tokens, 151936 x
-// 4096, G and the gradients: 64 / 128 / 256 MiB 13.6 / 13.9 / 14.2 ms, but 614 tokens of 1024,
-// 262144 x 2560: 3.31 / 3.15 with 64 / 128).
-constexpr int64_t kPieceBytes = int64_t(128) << 20;
+// Of G, and of a copy of the head's rows: some thousand tiles, so that a last round of 256 that
+// is not full costs little, and few additions to the hidden states' sums (64 / 128 / 256 MiB: G and the
+// gradients of 4096 tokens, 151936 x 4096 13.1 / 12.7 / 12.6 ms, of 614, 262144 x 2560 3.21 / 2.99 / 2.89).
+constexpr int64_t kPieceBytes = int64_t(256) << 20;
 constexpr int64_t kMaxTiles = int64_t(1) << 22;         // of a launch (its threads stay below 2^32)
 constexpr int kRBlock = 256;
 

@@ -236,6 +236,10 @@ extern "C" archead_status archead_rms_norm(const void* x, archead_dtype dtype, i
   if (!x || !weight || (!out && !codes) || (codes && !scales)) return fail(ARCHEAD_E_INVALID_ARG, "null pointer");
   if (ldx < d || (residual && ldr < d) || (total && ldt < d) || (out && ldo < d) || (codes && ldc < d))
     return fail(ARCHEAD_E_INVALID_ARG, "leading dimensions must be >= d");
+  // (in place each row only ever meets itself)
+  const auto moved = [&](const void* o, int64_t ld) { return o && ((o == x && ld != ldx) || (o == residual && ld != ldr)); };
+  if (moved(total, ldt) || moved(out, ldo)) return fail(ARCHEAD_E_INVALID_ARG, "in place, leading dimensions must agree");
+  if (total && total == out) return fail(ARCHEAD_E_INVALID_ARG, "total and out must be two");
   const int eb = dtype_bytes(dtype);
   if (!aligned(x, eb) || !aligned(residual, eb) || !aligned(total, eb) || !aligned(out, eb) ||
       !aligned(weight, dtype_bytes(weight_dtype)) || !aligned(scales, 4))

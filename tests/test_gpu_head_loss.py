@@ -100,7 +100,7 @@ def test_sharp_and_flat(M, V, d, sharp):
     _check(*i, *_step(*i))
 
 
-@pytest.mark.parametrize("M,V,d", [(4096, 33000, 64), (2100, 40000, 128), (5, 9001, 16383), (300, 8200, 16384)])
+@pytest.mark.parametrize("M,V,d", [(4096, 33000, 64), (2100, 70000, 128), (2100, 40000, 128), (5, 9001, 16383), (300, 8200, 16384)])
 def test_several_pieces(M, V, d):
     i = _inputs(M, V, d)
     _check(*i, *_step(*i))

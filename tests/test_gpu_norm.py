@@ -157,6 +157,10 @@ def test_norm_strides_and_places(dtype, d):
     _check(x, w, 1e-6, None, 0.0, out=out)
     vx.fill_(99)
     assert (bx == 99).all()
+    y, z = r.clone(), x.clone()
+    out, s = rms_norm(z, w, residual=y, total=z, out=y)
+    assert s is z and out is y
+    _check(x, w, 1e-6, r, 0.0, total=s, out=out)
     y = r.clone()
     out, s = rms_norm(x.clone(), w, residual=y, total=y)
     assert s is y

@@ -20,8 +20,8 @@ def L():
 
 
 def _norm(L, **kw):
-    a = dict(x=P, t=ab.BF16, M=2, d=64, ldx=64, r=P, ldr=64, w=P, wt=ab.BF16, off=0.0, eps=1e-6, total=P, ldt=64, out=P,
-             ldo=64, codes=P, ldc=64, scales=P)
+    a = dict(x=P, t=ab.BF16, M=2, d=64, ldx=64, r=2 * P, ldr=64, w=P, wt=ab.BF16, off=0.0, eps=1e-6, total=3 * P, ldt=64,
+             out=4 * P, ldo=64, codes=P, ldc=64, scales=P)
     a.update(kw)
     return L.archead_rms_norm(*a.values(), None)
 
@@ -39,6 +39,8 @@ def _norm(L, **kw):
     (dict(x=P + 1), ab.E_MISALIGNED), (dict(r=P + 1), ab.E_MISALIGNED), (dict(total=P + 1), ab.E_MISALIGNED),
     (dict(out=P + 1), ab.E_MISALIGNED), (dict(w=P + 1), ab.E_MISALIGNED), (dict(wt=ab.F32, w=P + 2), ab.E_MISALIGNED),
     (dict(t=ab.F32, wt=ab.F32, x=P + 2), ab.E_MISALIGNED), (dict(scales=P + 2), ab.E_MISALIGNED),
+    (dict(total=4 * P), ab.E_INVALID_ARG), (dict(total=P, ldt=65), ab.E_INVALID_ARG), (dict(total=2 * P, ldt=65), ab.E_INVALID_ARG),
+    (dict(out=P, ldo=65), ab.E_INVALID_ARG), (dict(out=2 * P, ldo=70), ab.E_INVALID_ARG),
 ])
 def test_norm_refusals(L, kw, status):
     assert _norm(L, **kw) == status, L.archead_last_error()
