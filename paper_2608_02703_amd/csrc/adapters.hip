@@ -139,17 +139,17 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, const f32x4
 // t[m, j] = scale sum_k x[m, k] a[j, k] in fp32, written as the second operands of
 // k_adapt_up's products.  A workgroup takes a tile of up to 16 tokens of one adapter (TT
 // neighbouring ones of it, which share the loads of a) and RC x 16 ranks, its WAVES waves pieces of K in turn, whose sums meet in LDS.  Both
-// operands come straight from memory (16 rows, all of a 128-byte line with two loads of
-// 16 bytes a lane: the order of k does not matter as long as both have the same), the
+// operands come straight from memory (16 rows of 64 bytes a load), the
 // ranks as the first.  Lanes past the tile's tokens or the adapter's ranks repeat the
-// first: their results are not used, and no load hangs on a branch.
+// first: their results are not used, and no load hangs on a branch.  8192 x 4096, 64 ranks
+// of 8 adapters: 59 us, 38 of them a's loads (10 grouping alone); 256 x 4096, up to 32 ranks of 32: 14 us.
 //
 // t goes through the matrix units in PARTS parts of the operands' type: two hold 17
 // bits of it in bf16 and 22 in fp16 (there after a power of two that brings a token's
 // largest of 32 ranks to 2^14, so that no part is below the normal numbers), three 25.
 template <int DT, int RC, int TOK, int PARTS, int WAVES, int TT>
-__global__ __launch_bounds__(64 * WAVES, TT == 1 ? 4 : 2) void k_adapt_down(AdaptArgs p) {
-  constexpr int STEPS = RC == 4 ? 4 : 8, PIECE = 32 * STEPS, ROW = RC * 16 + 4;
+__global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
+  constexpr int STEPS = TT == 2 ? 2 : RC == 4 ? 4 : 8, PIECE = 32 * STEPS, ROW = RC * 16 + 4;
   __shared__ Groups<TOK> g;
   __shared__ f32x4 part[WAVES][RC][64];
   __shared__ float ts[16 * ROW];
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * WAVES, TT == 1 ? 4 : 2) void k_adapt_down(Adap
       uint4 xv[STEPS][TT], av[STEPS][RC];
 #pragma unroll
       for (int j = 0; j < STEPS; ++j) {
-        const int at = 2 * (i * PIECE + 64 * (j / 2) + 16 * q + 8 * (j % 2));
+        const int at = 2 * (i * PIECE + 32 * j + 8 * q);
 #pragma unroll
         for (int u = 0; u < TT; ++u) xv[j][u] = load_any<uint4>(x[u] + at);
 #pragma unroll
@@ -316,7 +316,8 @@ __device__ __forceinline__ uint4 load_row(const uint8_t* row, int j, int R) {
 // (from memory, each wave for itself: 37 us more).  No load hangs
 // on a branch: lanes past a tile's tokens and ranks past the adapter's repeat others,
 // and are masked where they are used.  The last outputs of a row that is no multiple of
-// 64 go one by one.  Bound by y and out.
+// 64 go one by one.  Bound by y and out: 8192 x 14336 bf16 132 us (3.6 TB/s of the two),
+// 333 x 50257 fp32 35 (3.8 TB/s).
 template <int DT, int DY, int R32, int TOK, int PARTS, int BR, int TILES>
 __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_adapt_up(AdaptArgs p) {
   constexpr int YB = Eight<DY>::kBytes;
@@ -468,8 +469,8 @@ constexpr int parts_of(int x_dtype, int y_dtype) { return y_dtype == ARCHEAD_F32
 template <int DT, int TOK, int PARTS>
 hipError_t down(AdaptArgs p, const Shape& sh, hipStream_t s) {
   // Two tiles and 64 ranks to a workgroup where that leaves one for every CU (8192 x 4096, 64
-  // ranks of 8 adapters, one tile each: 63 us, 38 of them a's way through the L2s), else
-  // the least (fp16's powers of two are of 32).
+  // ranks of 8 adapters: one tile each 63 us, two 59), else the least (fp16's powers of two
+  // are of 32).
   const int r16 = (p.R + 15) / 16;
   const auto go = [&](auto k, int rc, int waves, int tt) {
     p.spread = int((sh.in_block + tt - 1) / tt);
