@@ -6,8 +6,9 @@ namespace {
 
 using namespace archead::rows;
 
-constexpr int kNShort = 512;         // longest row that 16 lanes take
-constexpr int64_t kNLongest = 16384;   // longest row of all: 1024 threads with two groups of 8, or 512 with four
+constexpr int kNHeld = 2;            // groups of 8 elements a thread holds
+constexpr int kNShort = 256;         // longest row that 16 lanes take
+constexpr int64_t kNLongest = 16384;   // longest row of all: 1024 threads
 
 struct NormArgs {
   const uint8_t* x;
@@ -65,16 +66,16 @@ __device__ __forceinline__ double lane_f64(double v, int l) {
 // s = x + r, t = s (offset + w), both rounded to fp32; 1 / sqrt(mean s^2 + eps)
 // scales t in the end, so the codes are those of t, whatever the norm: a rounding
 // of the norm never moves one.  SHORT: 16 lanes to a row, else a workgroup, as many
-// threads as hold it in HELD groups of 8 elements each (and one of the up to seven
+// threads as hold it in kNHeld groups of 8 elements each (and one of the up to seven
 // elements behind the last whole group); a workgroup takes rows one after another
 // and holds the weights.  The squares are summed in fp64: fp32 inputs may be so
 // large (or so small) that they leave fp32.  A row's t stays in registers, so every
 // element is read once and total may be where x or r are.  Bound by the bytes: 16384 x 8192
-// bf16 with every output 224 us (5.4 TB/s), 4096 x 2560 to 16 bits 15 (5.6 TB/s).
-template <int DT, bool W32, bool SHORT, int HELD>
-__global__ __launch_bounds__(SHORT ? 256 : kNLongest / 8 / HELD) void k_norm(NormArgs g) {
+// bf16 with every output 218 us (5.5 TB/s), 4096 x 2560 to 16 bits 15 (5.6 TB/s).
+template <int DT, bool W32, bool SHORT>
+__global__ __launch_bounds__(SHORT ? 256 : kNLongest / 8 / kNHeld) void k_norm(NormArgs g) {
   using E = Eight<DT>;
-  constexpr int WT = W32 ? int(ARCHEAD_F32) : DT, EB = E::kBytes, WB = Eight<WT>::kBytes;
+  constexpr int WT = W32 ? int(ARCHEAD_F32) : DT, EB = E::kBytes, WB = Eight<WT>::kBytes, HELD = kNHeld;
   static_assert(!SHORT || HELD * 128 == kNShort, "a short row is held whole");
   const int TPR = SHORT ? 16 : int(blockDim.x), rows = SHORT ? int(blockDim.x) / 16 : 1;
   __shared__ uint32_t smax[2][kNLongest / 8 / HELD / 64];
@@ -201,20 +202,21 @@ __global__ __launch_bounds__(SHORT ? 256 : kNLongest / 8 / HELD) void k_norm(Nor
   }
 }
 
-template <int DT, bool W32, bool SHORT, int HELD>
+template <int DT, bool W32, bool SHORT>
 hipError_t launch_rows(const NormArgs& g, hipStream_t s) {
-  const int64_t groups = SHORT ? (g.M + 15) / 16 : g.M, waves = SHORT ? 4 : (g.d + 512 * HELD - 1) / (512 * HELD);
+  const int64_t groups = SHORT ? (g.M + 15) / 16 : g.M, waves = SHORT ? 4 : (g.d + 512 * kNHeld - 1) / (512 * kNHeld);
   const int64_t most = 256 * (32 / waves > 0 ? 32 / waves : 1);   // workgroups that run at once, about
-  return launch_kernel(k_norm<DT, W32, SHORT, HELD>, dim3(unsigned(groups < most ? groups : most)),
+  return launch_kernel(k_norm<DT, W32, SHORT>, dim3(unsigned(groups < most ? groups : most)),
                        dim3(unsigned(64 * waves)), 0, s, g);
 }
 
-// (Fewer waves with more in flight each where there are plenty, as for the rounding of rows.)
+// Few waves with much in flight each gain nothing here (four groups a thread: 256 x 8192 bf16
+// 6.3 us, two 5.4; 8192 x 16384 201 and 177; 65536 x 1024 fp32 159 and 164).  16 lanes to a row
+// where they hold it as well (65536 rows of 128, 256: 15 and 23 us, a wave each 32 and 33; of 512
+// with four groups a thread 4096 rows 7.0 us, a wave each 5.8).
 template <int DT, bool W32>
 hipError_t launch_norm(const NormArgs& g, hipStream_t s) {
-  if (g.d <= kNShort) return launch_rows<DT, W32, true, 4>(g, s);
-  if (g.M * g.d < (1 << 25)) return launch_rows<DT, W32, false, 2>(g, s);
-  return launch_rows<DT, W32, false, 4>(g, s);
+  return g.d <= kNShort ? launch_rows<DT, W32, true>(g, s) : launch_rows<DT, W32, false>(g, s);
 }
 
 }  // namespace
