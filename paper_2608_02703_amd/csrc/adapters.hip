@@ -138,11 +138,12 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, const f32x4
 
 // t[m, j] = scale sum_k x[m, k] a[j, k] in fp32, written as the second operands of
 // k_adapt_up's products.  A workgroup takes a tile of up to 16 tokens of one adapter (TT
-// neighbouring ones of it, which share the loads of a) and RC x 16 ranks, its WAVES waves pieces of K in turn, whose sums meet in LDS.  Both
-// operands come straight from memory (16 rows of 64 bytes a load), the
-// ranks as the first.  Lanes past the tile's tokens or the adapter's ranks repeat the
-// first: their results are not used, and no load hangs on a branch.  8192 x 4096, 64 ranks
-// of 8 adapters: 59 us, 38 of them a's loads (10 grouping alone); 256 x 4096, up to 32 ranks of 32: 14 us.
+// neighbouring ones of it, which share the loads of a) and RC x 16 ranks, its WAVES waves
+// pieces of K in turn, whose sums meet in LDS.  Both operands come straight from memory
+// (16 rows of 64 bytes a load), the ranks as the first.  Lanes past the tile's tokens or the
+// adapter's ranks repeat the first: their results are not used, and no load hangs on a branch.  8192 x 4096, 64
+// ranks of 8 adapters: 63 us, 10 of them grouping, most of the rest a's way through the L2s;
+// 256 x 4096, up to 32 ranks of 32: 14 us, latency.
 //
 // t goes through the matrix units in PARTS parts of the operands' type: two hold 17
 // bits of it in bf16 and 22 in fp16 (there after a power of two that brings a token's
@@ -317,7 +318,7 @@ __device__ __forceinline__ uint4 load_row(const uint8_t* row, int j, int R) {
 // on a branch: lanes past a tile's tokens and ranks past the adapter's repeat others,
 // and are masked where they are used.  The last outputs of a row that is no multiple of
 // 64 go one by one.  Bound by y and out: 8192 x 14336 bf16 132 us (3.6 TB/s of the two),
-// 333 x 50257 fp32 35 (3.8 TB/s).
+// 333 x 50257 fp32 30 (4.5 TB/s).
 template <int DT, int DY, int R32, int TOK, int PARTS, int BR, int TILES>
 __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_adapt_up(AdaptArgs p) {
   constexpr int YB = Eight<DY>::kBytes;
@@ -457,6 +458,8 @@ struct Shape {
 };
 Shape shape(int64_t M, int64_t R, int64_t n) {
   Shape s{};
+  // (of 16 tokens both launches took 13.0 us in a block of 64, 15.1 in one of 256; of 256 in four
+  // blocks 26.7, in one 23.3)
   s.tok = M <= 64 ? 64 : 256;
   s.blocks = (M + s.tok - 1) / s.tok;
   const int64_t in = std::min<int64_t>(s.tok, M);
@@ -468,18 +471,23 @@ constexpr int parts_of(int x_dtype, int y_dtype) { return y_dtype == ARCHEAD_F32
 
 template <int DT, int TOK, int PARTS>
 hipError_t down(AdaptArgs p, const Shape& sh, hipStream_t s) {
-  // Two tiles and 64 ranks to a workgroup where that leaves one for every CU (8192 x 4096, 64
-  // ranks of 8 adapters: one tile each 63 us, two 59), else the least (fp16's powers of two
-  // are of 32).
+  // As many ranks to a workgroup as leave one for every CU, by the tiles that there may be, so
+  // that fewer load each x (4096 wide, both launches at N = 1024, 16 / 32 / 64 ranks a workgroup:
+  // 1024 tokens, 8 adapters of 64 ranks 29 / 29 / 35 us; 2048, 64 of 64 77 / 67 / 61; 8192, 64 of
+  // 64 230 / 172 / 155; 1024, 8 of 32 23 / 26).  Two tiles, which then share the loads of a, where
+  // most have a neighbour of their adapter (8192 tokens of 64 ranks, one tile and two: 1 adapter
+  // 61 and 47 us, 8 adapters 60 and 72).  fp16's powers of two are of 32 ranks.
   const int r16 = (p.R + 15) / 16;
   const auto go = [&](auto k, int rc, int waves, int tt) {
     p.spread = int((sh.in_block + tt - 1) / tt);
     return launch_kernel(k, dim3(unsigned(sh.blocks), unsigned((r16 + rc - 1) / rc), unsigned(p.spread)), dim3(64 * waves), 0, s, p);
   };
-  const int64_t full = (p.M + 15) / 16;   // tiles of tokens of one adapter each
-  if (r16 >= 3 && full / 2 * ((r16 + 3) / 4) >= 200) return go(k_adapt_down<DT, 4, TOK, PARTS, 8, 2>, 4, 8, 2);
+  const int64_t most = sh.blocks * sh.in_block;   // tiles
+  if constexpr (TOK == 256)
+    if (r16 >= 3 && p.n <= 4 && most * ((r16 + 3) / 4) >= 512) return go(k_adapt_down<DT, 4, TOK, PARTS, 8, 2>, 4, 8, 2);
+  if (r16 >= 3 && most * ((r16 + 3) / 4) >= 250) return go(k_adapt_down<DT, 4, TOK, PARTS, 8, 1>, 4, 8, 1);
   if constexpr (DT == ARCHEAD_F16) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 8, 1);
-  else if (r16 >= 2 && sh.blocks * sh.in_block * r16 / 2 >= 200) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 8, 1);
+  else if (r16 >= 2 && most * r16 / 2 >= 200) return go(k_adapt_down<DT, 2, TOK, PARTS, 8, 1>, 2, 8, 1);
   else return go(k_adapt_down<DT, 1, TOK, PARTS, 8, 1>, 1, 8, 1);
 }
 
@@ -488,12 +496,16 @@ hipError_t up(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
   const dim3 grid(unsigned((p.N + 64 * kUWaves - 1) / (64 * kUWaves)), unsigned((sh.in_block + TILES - 1) / TILES), unsigned(sh.blocks));
   return launch_kernel(k_adapt_up<DT, DY, R32, TOK, parts_of(DT, DY), BR, TILES>, grid, dim3(kUBlock), size_t(TILES) * sh.kcs * parts_of(DT, DY) * 1024, s, p);
 }
-// Four tiles to a wave (fp32 outputs two) where most tiles of a block are neighbours of
-// one adapter, one where most are of their own.
+// Four tiles to a wave (fp32 outputs two), which share b's rows where they are of one adapter,
+// where a block of 256 tokens may have whole tiles of each and the waves are plenty (one tile and
+// four: 8192 x 14336, 8 adapters of 64 ranks 257 and 219 us, 32 393 and 403, 128 1021 and 1088;
+// 2048 x 14336, 8 of 16 40.7 and 43.6; 4096 x 14336, 8 of 16 77 and 76).
 template <int DT, int DY, int R32, int TOK, int BR>
 hipError_t up_tiles(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
   constexpr int MANY = R32 <= 2 && DY != ARCHEAD_F32 ? 4 : 2;
-  return p.M >= 32 * p.n ? up<DT, DY, R32, TOK, BR, MANY>(p, sh, s) : up<DT, DY, R32, TOK, BR, 1>(p, sh, s);
+  if constexpr (TOK == 256)
+    if (p.n <= 16 && p.M * p.N >= (1 << 25)) return up<DT, DY, R32, TOK, BR, MANY>(p, sh, s);
+  return up<DT, DY, R32, TOK, BR, 1>(p, sh, s);
 }
 template <int DT, int DY, int TOK, int BR>
 hipError_t up_rank(const AdaptArgs& p, const Shape& sh, hipStream_t s) {
@@ -512,7 +524,11 @@ hipError_t up_type(const AdaptArgs& p, archead_dtype y, const Shape& sh, hipStre
 
 template <int DT, int TOK>
 hipError_t launch_tok(const AdaptArgs& p, archead_dtype y, const Shape& sh, hipStream_t s) {
-  const hipError_t e = parts_of(DT, y) == 3 ? down<DT, TOK, 3>(p, sh, s) : down<DT, TOK, 2>(p, sh, s);
+  hipError_t e;
+  if constexpr (DT == ARCHEAD_BF16)
+    e = parts_of(DT, y) == 3 ? down<DT, TOK, 3>(p, sh, s) : down<DT, TOK, 2>(p, sh, s);
+  else
+    e = down<DT, TOK, 2>(p, sh, s);
   if (e != hipSuccess) return e;
   return p.R % 8 == 0 ? up_type<DT, TOK, kEights>(p, y, sh, s)
          : p.R > 8    ? up_type<DT, TOK, kOver>(p, y, sh, s)
