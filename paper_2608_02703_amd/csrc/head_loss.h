@@ -15,7 +15,9 @@ constexpr int kRowPad = 256;       // buffers hold this many tokens' rows or a m
 // The products, out[i, j] = sum_k: 
 //   kStats   i token, j vocabulary row, k of d: a tile's largest logit and sum of
 //            exponentials per token, and the target's logit
-//   kGrad    the same logits, as G = g (exp(l - lse) - [j = target]) in bf16
+//   kGrad    the same logits, as G = g (exp(l - lse) - [j = target]) in bf16, the operand
+//            of the matrix units below: 2^-9 of each entry, independent of one another,
+//            so less of a sum of many (fp32 entries would be two operands, twice the products)
 //   kHidden  i token, j of d, k vocabulary row: sums of G w into fp32
 //   kHead    i vocabulary row, j of d, k token: rows of G^T x in bf16
 enum Op { kStats, kGrad, kHidden, kHead };

@@ -17,7 +17,6 @@ constexpr int64_t kMaxLdw = int64_t(1) << 20;           // a tile's rows stay wi
 // is not full costs little, and few additions to the hidden states' sums (64 / 128 / 256 MiB: G and the
 // gradients of 4096 tokens, 151936 x 4096 13.1 / 12.7 / 12.6 ms, of 614, 262144 x 2560 3.21 / 2.99 / 2.89).
 constexpr int64_t kPieceBytes = int64_t(256) << 20;
-constexpr int64_t kMaxTiles = int64_t(1) << 22;         // of a launch (its threads stay below 2^32)
 constexpr int kRBlock = 256;
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -175,28 +174,13 @@ __global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int64_
   const int64_t split_step = padded_rows(live) * dp;
   typedef float f32x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-  // many parts: a quarter of them to each wave
-  __shared__ f32x8 met[kRBlock / 64][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const bool shared = splits >= 8;
-  for (int64_t j0 = shared ? 0 : 512 * wave; j0 < d; j0 += shared ? 512 : 512 * (kRBlock / 64)) {
-    const int64_t j = j0 + 8 * lane;
+  for (int64_t j = 8 * threadIdx.x; j < d; j += 8 * kRBlock) {
     f32x8 v = {};
-    if (p >= 0 && j < d) {
+    if (p >= 0) {
       const float* const from = sums + p * dp + j;
 #pragma unroll 4
-      for (int s = shared ? wave : 0; s < splits; s += shared ? kRBlock / 64 : 1)
-        v += *reinterpret_cast<const f32x8*>(from + s * split_step);
+      for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x8*>(from + s * split_step);
     }
-    if (shared) {
-      met[wave][lane] = v;
-      __syncthreads();
-      if (wave == 0)
-        for (int w = 1; w < kRBlock / 64; ++w) v += met[w][lane];
-      __syncthreads();
-      if (wave != 0) continue;
-    }
-    if (j >= d) continue;
     const bf16x8 o = __builtin_convertvector(v, bf16x8);
     uint16_t* const to = dx + m * ld + j;
     if (j + 8 <= d) {
@@ -255,7 +239,6 @@ Plan plan(int64_t M, int64_t V, int64_t d, bool direct, bool grad) {
   p.piece = up(V, kTileJ);
   if (!direct) p.piece = std::min(p.piece, std::max<int64_t>(kTileJ, kPieceBytes / (p.dp * 2) / kTileJ * kTileJ));
   if (grad) p.piece = std::min(p.piece, std::max<int64_t>(16 * kTileJ, kPieceBytes / (p.Mp * 2) / kTileJ * kTileJ));
-  p.piece = std::min(p.piece, kTileJ * std::max<int64_t>(1, kMaxTiles / ((M + 63) / 64)));
   p.ti = rows_of_tiles(M, up(p.piece, kTileJ) / kTileJ, 64);
   p.ti_x = rows_of_tiles(M, 1 << 20, 64);   // (its parts of k fill the CUs)
   p.ti_w = rows_of_tiles(std::min(V, p.piece), up(d, kTileJ) / kTileJ, 128);
