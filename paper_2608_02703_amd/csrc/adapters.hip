@@ -249,7 +249,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
         top = fmaxf(top, __shfl_xor(top, 32));
         int e = 15;
         if (top > 0 && top < INFINITY) frexpf(top, &e);
-        e = max(-100, min(100, 15 - e));
+        e = min(126, 15 - e);   // (no less than -113; 2^-126 is the least that back holds)
         pre = ldexpf(1.f, e);
         if (ql == 0) p.back[((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * 16 + (w & 15)] = ldexpf(1.f, -e);
       }

@@ -229,3 +229,17 @@ def test_beyond_32_bit_offsets():
     _check(i, adapters_add(**j))
     adapters_add(**j, out=y)
     _check(i, y)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 117, 2.0 ** -95])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_largest_and_smallest_scales(scale, dtype):
+    """Inner sums near the ends of fp32: they keep their bits, and reach the sum finite.
+    (Three bf16 parts of 2^-95 are normal numbers down to 2^-14 of it.)"""
+    from paper_2608_02703_amd import adapters_add
+    i = _inputs(20, 70, 64, 40, 3, dtype, "f32", seed=9)
+    i["y"].zero_()
+    i["scales"] = torch.tensor([scale, -scale, scale / 2], device="cuda")
+    out = adapters_add(**i)
+    assert torch.isfinite(out).all()
+    _check(i, out)
