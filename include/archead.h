@@ -663,9 +663,9 @@ archead_status archead_rms_norm(const void* x, archead_dtype dtype, int64_t M, i
  *   G[m, v]  = grad[m] (exp(logit[v] - lse[m]) - [v = y])
  *   dx[m, :] = sum_v G[m, v] w[v, :],      dw[v, :] = sum_m G[m, v] x[m, :]
  * grad[m] is what the loss of token m counts for in the whole (1 / M for a
- * mean).  G is rounded to bf16 for its products (its entries, and
- * exponentials, below 2^-126 count as 0), whose sums are fp32; dx and dw are
- * rounded to bf16 once.  A token whose target lies outside [0, V) (say
+ * mean).  G is rounded to bf16 for its products, in units of the largest finite
+ * |grad| (its entries there, and exponentials, below 2^-126 count as 0), whose sums
+ * are fp32; dx and dw are rounded to bf16 once.  A token whose target lies outside [0, V) (say
  * -100) has loss 0, lse 0 and dx 0 and adds nothing to dw, whatever its row of x
  * and its grad hold; it costs no products.  A token whose logits hold a NaN or +inf gets
  * NaN. */

@@ -16,8 +16,10 @@ constexpr int kRowPad = 256;       // buffers hold this many tokens' rows or a m
 //   kStats   i token, j vocabulary row, k of d: a tile's largest logit and sum of
 //            exponentials per token, and the target's logit
 //   kGrad    the same logits, as G = g (exp(l - lse) - [j = target]) in bf16, the operand
-//            of the matrix units below: 2^-9 of each entry, independent of one another,
-//            so less of a sum of many (fp32 entries would be two operands, twice the products)
+//            of the matrix units below, g in units of the largest: up to 2^-8 of each entry,
+//            independent of one another, so less of a sum of many, and next to nothing at
+//            the targets of tokens that count alike (fp32 entries would be two operands,
+//            twice the products)
 //   kHidden  i token, j of d, k vocabulary row: sums of G w into fp32
 //   kHead    i vocabulary row, j of d, k token: rows of G^T x in bf16
 enum Op { kStats, kGrad, kHidden, kHead };
@@ -39,7 +41,8 @@ struct TileArgs {
   // kGrad
   const int32_t* target;   // [token]
   const float* lse;        // [token]
-  const float* g;          // [token]
+  const float* g;          // [token], in units of the largest
+  const float* unit;       // kHead: of g
   uint16_t* out;           // kGrad: G [token][out_ld]; kHead: dw
   int64_t out_ld;
   // kHidden

@@ -33,7 +33,8 @@ struct RowArgs {
   int32_t* pos;            // [M] place among the live tokens, or -1
   int32_t* y;              // [Mp] by place
   float* lse_out;
-  float* g_out;
+  float* g_out;            // in units of *unit
+  float* unit;             // the largest finite |g| of a live token
   uint16_t* rows;          // [Mp][x_ld]
 };
 
@@ -46,32 +47,48 @@ __device__ __forceinline__ int64_t target_of(const RowArgs& a, int64_t m) {
 // order, with zeros behind each row up to whole stages and behind the last token's
 // for sums over tokens: tokens without a target cost no products, and nothing that
 // their rows hold can reach a sum.  Each workgroup counts the live tokens before its own.
+// g goes on in units of the largest, which the gradients get back in fp32: the entries of G
+// that weigh most, g (p - 1) at the targets, are then -1 + p for tokens that count alike, and
+// lose next to nothing in bf16 (g itself, say 1 / 87, would lose up to 2^-8 in each of them).
 __global__ __launch_bounds__(kRBlock) void k_ce_rows(RowArgs a) {
   __shared__ int32_t sums[2][kRBlock / 64], place[kRBlock];
+  __shared__ float tops[kRBlock / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t first = int64_t(blockIdx.x) * a.per_block, end = std::min(a.M, first + a.per_block);
   int before = 0, all = 0;
+  float unit = 0;
   for (int64_t m = tid; m < a.M; m += kRBlock) {
     const bool live = target_of(a, m) >= 0;
     all += live;
     before += live && m < first;
+    if (live && a.lse) {
+      const float g = fabsf(a.g[m]);
+      if (g < INFINITY) unit = fmaxf(unit, g);
+    }
   }
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
     before += __shfl_xor(before, s);
     all += __shfl_xor(all, s);
+    unit = fmaxf(unit, __shfl_xor(unit, s));
   }
   if (lane == 0) {
     sums[0][wave] = before;
     sums[1][wave] = all;
+    tops[wave] = unit;
   }
   __syncthreads();
   before = all = 0;
   for (int w = 0; w < kRBlock / 64; ++w) {
     before += sums[0][w];
     all += sums[1][w];
+    unit = fmaxf(unit, tops[w]);
   }
-  if (blockIdx.x == 0 && tid == 0) *a.count = all;
+  if (unit == 0) unit = 1;
+  if (blockIdx.x == 0 && tid == 0) {
+    *a.count = all;
+    *a.unit = unit;
+  }
   const int groups = int(a.dp / 8);
   for (int64_t m0 = first; m0 < end; m0 += kRBlock) {
     const int64_t m = m0 + tid;
@@ -91,7 +108,7 @@ __global__ __launch_bounds__(kRBlock) void k_ce_rows(RowArgs a) {
       a.y[at] = int32_t(y);
       if (a.lse) {
         a.lse_out[at] = a.lse[m];
-        a.g_out[at] = a.g[m];
+        a.g_out[at] = a.g[m] / unit;
       }
     }
     __syncthreads();
@@ -167,13 +184,14 @@ __global__ __launch_bounds__(kRBlock) void k_ce_merge(const float2* part, int64_
 // The gradient of a token's hidden state from the parts of its sums, zeros for a
 // token without a target.
 __global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int64_t sum_rows, int64_t first_stages, int ti, int64_t dp,
-                                                       const int32_t* count, const int32_t* pos, int64_t d, uint16_t* dx, int64_t ld) {
+                                                       const int32_t* count, const float* unit, const int32_t* pos, int64_t d, uint16_t* dx, int64_t ld) {
   const int64_t m = blockIdx.x;
   const int p = pos[m], live = *count;
   const int splits = splits_for((live + ti - 1) / ti * ((d + kTileJ - 1) / kTileJ), live, sum_rows, first_stages);
   const int64_t split_step = padded_rows(live) * dp;
   typedef float f32x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+  const float c = *unit;
   for (int64_t j = 8 * threadIdx.x; j < d; j += 8 * kRBlock) {
     f32x8 v = {};
     if (p >= 0) {
@@ -181,7 +199,7 @@ __global__ __launch_bounds__(kRBlock) void k_ce_hidden(const float* sums, int64_
 #pragma unroll 4
       for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x8*>(from + s * split_step);
     }
-    const bf16x8 o = __builtin_convertvector(v, bf16x8);
+    const bf16x8 o = __builtin_convertvector(v * c, bf16x8);
     uint16_t* const to = dx + m * ld + j;
     if (j + 8 <= d) {
       store_any(to, o);
@@ -254,7 +272,7 @@ Plan plan(int64_t M, int64_t V, int64_t d, bool direct, bool grad) {
     at += (bytes + 255) / 256 * 256;
     return o;
   };
-  p.count = take(4);
+  p.count = take(8);   // and the unit of g
   p.pos = take(M * 4);
   p.y = take(p.Mp * 4);
   p.rows = take(p.Mp * p.x_ld * 2);
@@ -306,6 +324,7 @@ hipError_t gather(const Plan& p, char* ws, const void* x, int64_t ldx, const voi
   a.per_block = int(std::max<int64_t>(4, (p.M + 1023) / 1024));
   a.t64 = tdt == ARCHEAD_I64;
   a.count = reinterpret_cast<int32_t*>(ws + p.count);
+  a.unit = reinterpret_cast<float*>(a.count + 1);
   a.pos = reinterpret_cast<int32_t*>(ws + p.pos);
   a.y = reinterpret_cast<int32_t*>(ws + p.y);
   a.lse_out = reinterpret_cast<float*>(ws + p.lse);
@@ -412,6 +431,7 @@ extern "C" archead_status archead_head_loss_grad(const void* x, int64_t ldx, con
     }
     if (dw && e == hipSuccess) {
       q = t;
+      q.unit = reinterpret_cast<const float*>(t.count + 1);
       q.a = G, q.a_ld = p.g_ld, q.b = t.a, q.b_ld = t.a_ld, q.rows = t.cols, q.cols = d;
       q.out = static_cast<uint16_t*>(dw) + v0 * lddw, q.out_ld = lddw;
       e = launch_tiles(kHead, p.ti_w, q, s);
@@ -419,6 +439,7 @@ extern "C" archead_status archead_head_loss_grad(const void* x, int64_t ldx, con
   }
   if (dx && e == hipSuccess)
     e = launch_kernel(k_ce_hidden, dim3(unsigned(M)), dim3(kRBlock), 0, s, sums, p.sum_rows, p.first_stages, p.ti_x, p.dp,
-                      reinterpret_cast<const int32_t*>(base + p.count), reinterpret_cast<const int32_t*>(base + p.pos), d, static_cast<uint16_t*>(dx), lddx);
+                      reinterpret_cast<const int32_t*>(base + p.count), reinterpret_cast<const float*>(base + p.count + 4),
+                      reinterpret_cast<const int32_t*>(base + p.pos), d, static_cast<uint16_t*>(dx), lddx);
   return launch_status(e, "head gradient launch");
 }

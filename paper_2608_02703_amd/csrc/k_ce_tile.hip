@@ -433,6 +433,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
       const int64_t row0 = i0 + wi * NI * 32 + 32 * i, token = row0 + lr;
       float lse = 0, gr = 0;
       int y = -1;
+      const float unit = OP == kHead ? *g.unit : 1.f;
       if constexpr (OP == kGrad) {
         if (token < live) {
           lse = g.lse[token];
@@ -452,6 +453,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             v[e] = acc[i][j][4 * k + e];
+            if constexpr (OP == kHead) v[e] *= unit;
             if constexpr (OP == kGrad) {
               const int c = 32 * j + 8 * k + 4 * h + e;
               float p = __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, base));

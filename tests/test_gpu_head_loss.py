@@ -245,3 +245,46 @@ def test_repeatable_streams_and_graphs():
         torch.cuda.synchronize()
         want = _step(x, w, targets, grad)
         assert all(torch.equal(a, b) for a, b in zip((loss, lse, dx, dw), want))
+
+
+@pytest.mark.parametrize("M", [87, 300])
+def test_a_mean_loses_no_more_than_its_outputs_do(M):
+    """grad 1 / M, which bf16 does not hold: G is in units of it, its entry at a target
+    -(1 - p), off by half a step of 2^-8 at most, and by p where it
+    rounds to 1; its others are off by 2^-8 p each.
+    The rest are the sums' errors and two products' by the unit, and half a step of the output."""
+    V, d = 4096, 128
+    x, w, targets, _ = _inputs(M, V, d, ignored=0.0)
+    x = (x.float() * 0.5).bfloat16()
+    grad = torch.full((M,), 1 / M, device="cuda")
+    loss, lse, dx, dw = _step(x, w, targets, grad)
+    o = oracle.head_loss(x, w, targets, grad)
+    tg = _tols(o, V, d)[2]
+    xs, ws = x.double(), w.double()
+    p = torch.exp(xs @ ws.t().contiguous() - o["lse"][:, None])
+    off = R * p
+    off[torch.arange(M), targets] = p[torch.arange(M), targets].clamp(max=2.0 ** -9)
+    off *= grad[0].double() * (1 + 2.0 ** -7)
+
+    def half_step(v):   # of bf16 at v
+        return torch.ldexp(torch.ones_like(v), torch.frexp(v)[1] - 9)
+    least = 2.0 ** -120
+    tx = off @ ws.abs() + (tg[:, None] + (V + 2) * U) * o["dx_mag"] + least
+    _within(dx, o["dx"], tx + half_step(o["dx"].abs() + tx), "dx")
+    tw = off.t().contiguous() @ xs.abs() + (tg.max() + (M + 2) * U) * o["dw_mag"] + least
+    _within(dw, o["dw"], tw + half_step(o["dw"].abs() + tw), "dw")
+
+
+@pytest.mark.parametrize("odd", [0.0, float("inf"), 2.0 ** -140, 2.0 ** 100])
+def test_grads_of_any_size(odd):
+    """All zero, one without a bound, all below the normal numbers, and large ones."""
+    x, w, targets, _ = _inputs(40, 300, 64, ignored=0.0)
+    grad = torch.full((40,), 0.5 if odd == float("inf") else odd, device="cuda")
+    if odd == float("inf"):
+        grad[3] = odd
+    loss, lse, dx, dw = _step(x, w, targets, grad)
+    if odd == float("inf"):
+        assert not torch.isfinite(dx[3]).any() and torch.isfinite(dx[:3]).all() and torch.isfinite(dx[4:]).all()
+        assert not torch.isfinite(dw).all()
+    else:
+        _check(x, w, targets, grad, loss, lse, dx, dw)
