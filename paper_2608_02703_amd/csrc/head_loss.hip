@@ -175,9 +175,9 @@ __global__ __launch_bounds__(kRBlock) void k_ce_merge(const float2* part, int64_
     }
   }
   if (lane == 0) {
-    const float l = p >= 0 ? top + logf(sum) : 0.f;
-    lse[m] = l;
-    loss[m] = p >= 0 ? l - at_target[p] : 0.f;
+    const float log_sum = logf(sum);
+    lse[m] = p >= 0 ? top + log_sum : 0.f;
+    loss[m] = p >= 0 ? top - at_target[p] + log_sum : 0.f;   // (lse's rounding would be most of a small loss's error)
   }
 }
 
