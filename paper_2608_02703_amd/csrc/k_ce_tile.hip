@@ -272,9 +272,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
   // operands are read and the loads of the one after overwrite this one, all under
   // the last step's products.
   //
-  // 4096 x 151936 x 4096 (5.1 Tflop each): logits 3.74 to 3.9 ms (1.36 to 1.31 Pflop/s; the matrix
-  // units are busy 69 % of the time at the 1.74 GHz that the power limit leaves), G 4.37,
-  // hidden states 3.90, head 4.13.
+  // 4096 x 151936 x 4096 (5.1 Tflop each): logits 3.74 to 4.0 ms over cards (1.36 to 1.27
+  // Pflop/s; the matrix units are busy 69 % of the time at the 1.74 GHz that the power limit
+  // leaves), G 4.3 to 4.6, hidden states 3.8 to 4.0, head 4.1 to 4.3.
   if (all_stages > 0) {
     begin();
 #pragma unroll
