@@ -476,7 +476,8 @@ hipError_t down(AdaptArgs p, const Shape& sh, hipStream_t s) {
   // 1024 tokens, 8 adapters of 64 ranks 29 / 29 / 35 us; 2048, 64 of 64 77 / 67 / 61; 8192, 64 of
   // 64 230 / 172 / 155; 1024, 8 of 32 23 / 26).  Two tiles, which then share the loads of a, where
   // most have a neighbour of their adapter (8192 tokens of 64 ranks, one tile and two: 1 adapter
-  // 61 and 47 us, 8 adapters 60 and 72).  fp16's powers of two are of 32 ranks.
+  // 61 and 47 us, 8 adapters in any order 60 and 72, in runs of tokens 63 and 60 alone).  fp16's
+  // powers of two are of 32 ranks.
   const int r16 = (p.R + 15) / 16;
   const auto go = [&](auto k, int rc, int waves, int tt) {
     p.spread = int((sh.in_block + tt - 1) / tt);
