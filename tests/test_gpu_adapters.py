@@ -243,3 +243,15 @@ def test_largest_and_smallest_scales(scale, dtype):
     out = adapters_add(**i)
     assert torch.isfinite(out).all()
     _check(i, out)
+
+
+@pytest.mark.parametrize("dtype,y", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("M,N,K,R,n", [(2100, 40, 100, 256, 2), (2100, 33, 264, 200, 4), (700, 50, 72, 90, 300),
+                                       (64, 40, 136, 256, 70), (1100, 30601, 40, 20, 3), (1100, 30600, 33, 70, 16)])
+def test_many_tokens(M, N, K, R, n, dtype, y):
+    """Enough tokens, or outputs, for the ways that take more ranks or tiles at a time, their ids in runs and not."""
+    from paper_2608_02703_amd import adapters_add
+    i = _inputs(M, N, K, R, n, dtype, y, seed=M + N, ragged=n % 2 == 0)
+    if n <= 4:
+        i["ids"][:M // 2] = i["ids"][:M // 2].sort().values
+    _check(i, adapters_add(**i))
