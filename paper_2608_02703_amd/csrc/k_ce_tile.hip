@@ -366,11 +366,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
       top = fmaxf(top, __shfl_xor(top, 32));
       if (top > -INFINITY) {
-        const float base = -top * kLog2e;   // (rounded once for all of a token: 2^-24 of top in the tile's log sum)
+        // (subtracted before it is scaled: the largest's exponential is 1 whatever its size, and
+        // finite logits of any size have finite sums)
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, base));
+          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - top) * kLog2e);
       } else {
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
