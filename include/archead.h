@@ -668,7 +668,8 @@ archead_status archead_rms_norm(const void* x, archead_dtype dtype, int64_t M, i
  * are fp32; dx and dw are rounded to bf16 once.  A token whose target lies outside [0, V) (say
  * -100) has loss 0, lse 0 and dx 0 and adds nothing to dw, whatever its row of x
  * and its grad hold; it costs no products.  A token whose logits hold a NaN or +inf gets
- * NaN. */
+ * NaN.  lse is fp32, so the gradients' exponentials are off by up to 2^-24 |lse| of them;
+ * the loss is formed beside it, and has no such error. */
 
 /* Bytes of device workspace of the calls below (grad: 0 for archead_head_loss,
  * 1 for archead_head_loss_grad; 0 for M < 1 or sizes that the calls refuse).

@@ -444,7 +444,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
       }
       b16x4 out[NJ][4];
-      const float base = -lse * kLog2e;
       const bool some = token < live;
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -457,7 +456,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
             if constexpr (OP == kHead) v[e] *= unit;
             if constexpr (OP == kGrad) {
               const int c = 32 * j + 8 * k + 4 * h + e;
-              float p = __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, base));
+              float p = __builtin_amdgcn_exp2f((v[e] - lse) * kLog2e);   // (scaled first it would leave fp32)
               if (y == c) p -= 1.f;
               v[e] = some && (whole || jw + c < cols) ? p * gr : 0.f;
             }
