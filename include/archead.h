@@ -631,7 +631,8 @@ archead_status archead_matmul_i8(const int8_t* a, int64_t lda, const float* a_sc
  * so codes * scales is out to 8 bits, and feeds archead_matmul_i8.  (out is
  * formed from t and 1 / n rounded to fp32: off by at most 2^-23 of it before
  * its rounding.)  A row whose t holds an infinity or a NaN gets out and scale
- * NaN and codes 0.
+ * NaN and codes 0; one whose t are all 0 a scale of 2^-126 / n, or the largest
+ * finite number if that is less.
  *   x         fp32, bf16 or fp16 (dtype) [M, ldx] device, 1 <= d <= 16384
  *   residual  dtype [M, ldr] device or NULL
  *   weight    dtype or fp32 [d] device;  offset  0, or 1 for weights held as

@@ -1,5 +1,7 @@
 // archead_rms_norm: the residual's addition, the root-mean-square norm of rows,
 // and their rounding to 8 bits.
+#include <cfloat>
+
 #include "dev_codes.cuh"
 
 namespace {
@@ -174,9 +176,11 @@ __global__ __launch_bounds__(SHORT ? 256 : kNLongest / 8 / kNHeld) void k_norm(N
     const bool finite = top < 0x7f800000u;
     const double rs = finite ? 1.0 / sqrt(sum / double(g.d) + g.eps) : double(NAN);
     if (g.out) {
-      // rows so large that 1 / norm is below fp32's normal numbers: t is made smaller first
-      const bool large = rs < 0x1p-100;
-      const float pre = large ? 0x1p-40f : 1.f, by = float(large ? rs * 0x1p40 : rs);
+      // where 1 / norm leaves fp32's normal numbers a power of two goes to t instead: t is at most
+      // 2^7 norm times the weight, and above 2^156 (an eps below 2^-312) every x is 0
+      const bool large = rs < 0x1p-100, small = rs > 0x1p100;
+      const float pre = large ? 0x1p-40f : small ? 0x1p64f : 1.f;
+      const float by = float(large ? rs * 0x1p40 : small ? fmin(rs * 0x1p-64, 0x1p120) : rs);
       uint8_t* const out = g.out + m * g.o_row;
 #pragma unroll
       for (int h = 0; h < HELD; ++h) {
@@ -190,7 +194,7 @@ __global__ __launch_bounds__(SHORT ? 256 : kNLongest / 8 / kNHeld) void k_norm(N
     if (g.codes) {
       const float u = finite ? fmaxf(__uint_as_float(top) / 127.f, 0x1p-126f) : 1.f, inv = 1.f / u;
       int8_t* const codes = g.codes + m * g.ldc;
-      if (t == 0) g.scales[m] = float(double(u) * rs);
+      if (t == 0) g.scales[m] = top ? float(double(u) * rs) : float(fmin(double(u) * rs, double(FLT_MAX)));
 #pragma unroll
       for (int h = 0; h < HELD; ++h)
         if (at(h) < nd) store_any(codes + at(h), codes8(v[h], u, inv, finite));
