@@ -11,6 +11,7 @@ using namespace archead::rows;
 constexpr int kUBlock = 256, kUWaves = kUBlock / 64;   // threads and waves of the outer products' workgroups
 constexpr int64_t kMaxRank = 256;
 constexpr int64_t kMaxM = int64_t(1) << 23;
+constexpr float kMostBf16 = 0x1.fep127f;   // the largest finite bf16
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -262,7 +263,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
           uint16_t bits;
           float now;
           if constexpr (DT == ARCHEAD_BF16) {
-            const __bf16 h = __bf16(rest);
+            // (finite ones that would round to an infinity leave more to the next part)
+            const __bf16 h = __bf16(fabsf(rest) < INFINITY ? fminf(fmaxf(rest, -kMostBf16), kMostBf16) : rest);
             now = float(h);
             __builtin_memcpy(&bits, &h, 2);
           } else {
