@@ -714,8 +714,9 @@ archead_status archead_head_loss_grad(const void* x, int64_t ldx, const void* w,
  * and out[m, :] = y[m, :] where i lies outside [0, n): a token without an
  * adapter (its x is not read).  Products of 16-bit numbers, sums in fp32: the
  * inner sums are held in fp32 and go into the outer ones to 17 bits or more (24
- * for bf16 x with fp32 y, 22 for fp16 x; fewer where they are below 2^-100), and out is
- * rounded to y's type once. */
+ * for bf16 x with fp32 y, 22 for fp16 x; fewer where they are below 2^-100), each
+ * whatever the token's others are, and out is rounded to y's type once.  An infinity or
+ * NaN in b makes the outputs that it goes into infinite or NaN. */
 typedef struct archead_adapters {
   const void* a;            /* x's type: adapter i's a_i [R, K] at i * a_adapter, rows a_row apart */
   const void* b;            /* x's type: b_i [N, R] at i * b_adapter, rows b_row apart (all in elements) */

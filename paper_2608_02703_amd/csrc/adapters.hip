@@ -28,7 +28,7 @@ struct AdaptArgs {
   const int32_t* ranks;    // may be null
   uint8_t* out;
   uint4* t;                // operands [block][tile][32 ranks][part][64 lanes]
-  float* back;             // fp16: powers of two [block][tile][32 ranks][16 tokens]
+  float* back;             // fp16: powers of two [block][tile][32 ranks][16 tokens], or -1: t is in fp32
   uint8_t* table;          // Groups of the blocks
   int64_t M, N, K, n;
   int64_t y_row, x_row, a_ad, a_row, b_ad, b_row, o_row;   // bytes
@@ -148,7 +148,9 @@ __device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, const f32x4
 //
 // t goes through the matrix units in PARTS parts of the operands' type: two hold 17
 // bits of it in bf16 and 22 in fp16 (there after a power of two that brings a token's
-// largest of 32 ranks to 2^14, so that no part is below the normal numbers), three 25.
+// largest of 32 ranks to 2^14), three 25.  fp16's two have 22 bits of sums from 2^-3 on, 2^-17 of
+// the largest.  Where one of a tile's is less, and not 0 (of normally distributed sums in a tile of
+// some two hundred), its 32 ranks go on in fp32, in the place of two parts.
 template <int DT, int RC, int TOK, int PARTS, int WAVES, int TT>
 __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
   constexpr int STEPS = TT == 2 ? 2 : RC == 4 ? 4 : 8, PIECE = 32 * STEPS, ROW = RC * 16 + 4;
@@ -245,14 +247,20 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
         v[i] = ts[(w & 15) * ROW + jl + i];
         top = fmaxf(top, fabsf(v[i]));
       }
+      bool full = false;   // of a tile's 32 ranks, which a wave has
       if constexpr (DT == ARCHEAD_F16) {
+        static_assert(RC >= 2, "a wave has 32 ranks");
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         int e = 15;
         if (top > 0 && top < INFINITY) frexpf(top, &e);
         e = min(126, 15 - e);   // (no less than -113; 2^-126 is the least that back holds)
         pre = ldexpf(1.f, e);
-        if (ql == 0) p.back[((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * 16 + (w & 15)] = ldexpf(1.f, -e);
+        bool small = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) small |= v[i] != 0 && fabsf(v[i] * pre) < 0x1p-3f;
+        full = __ballot(small) != 0;
+        if (ql == 0) p.back[((int64_t(blockIdx.x) * p.per_block + ti) * p.kcs + kc) * 16 + (w & 15)] = full ? -1.f : ldexpf(1.f, -e);
       }
       uint32_t bits4[PARTS][4] = {};
 #pragma unroll
@@ -275,6 +283,11 @@ __global__ __launch_bounds__(64 * WAVES, 4) void k_adapt_down(AdaptArgs p) {
           bits4[k][i / 2] |= uint32_t(bits) << (16 * (i & 1));
           rest = fabsf(now) < INFINITY ? rest - now : 0.f;   // (an infinity or NaN has no rest)
         }
+      }
+      if (DT == ARCHEAD_F16 && full) {
+        static_assert(DT != ARCHEAD_F16 || PARTS == 2, "eight fp32 take two parts' place");
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bits4[i / 4][i % 4] = __float_as_uint(v[i]);
       }
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) {
@@ -320,9 +333,11 @@ __device__ __forceinline__ uint4 load_row(const uint8_t* row, int j, int R) {
 // on a branch: lanes past a tile's tokens and ranks past the adapter's repeat others,
 // and are masked where they are used.  The last outputs of a row that is no multiple of
 // 64 go one by one.  Bound by y and out: 8192 x 14336 bf16 132 us (3.6 TB/s of the two),
-// 333 x 50257 fp32 30 (4.5 TB/s).
+// 333 x 50257 fp32 30 (4.5 TB/s).  The way of t in fp32 costs fp16 up to 4 % in registers (both
+// launches, 8192 x 14336 of 8 x 64 ranks 201 and 208 us); with up to 32 ranks and four tiles, three waves
+// of a SIMD hold what four spill (12 ranks 176 us, so 167).
 template <int DT, int DY, int R32, int TOK, int PARTS, int BR, int TILES>
-__global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_adapt_up(AdaptArgs p) {
+__global__ __launch_bounds__(kUBlock, R32 == 1 && DT == ARCHEAD_F16 && TILES > 1 ? 3 : R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_adapt_up(AdaptArgs p) {
   constexpr int YB = Eight<DY>::kBytes;
   const int lane = threadIdx.x & 63, lr = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -393,18 +408,29 @@ __global__ __launch_bounds__(kUBlock, R32 <= 2 ? 4 : R32 == 4 ? 2 : 1) void k_ad
           w = uint4{d[0], d[1], d[2], d[3]};
         }
       }
+      float by = 1;
+      if constexpr (DT == ARCHEAD_F16) by = p.back[op * 16 + lr];
+      if (DT == ARCHEAD_F16 && __builtin_expect(int(__builtin_amdgcn_readfirstlane(__float_as_uint(by))) < 0, 0)) {
+        // t in fp32: products of fp32, of the ranks 8 q + i in turn
+        by = 1;
+        Eight<ARCHEAD_F32> t;
+        t.w[0] = tv[0], t.w[1] = tv[1];
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k)
+        for (int c = 0; c < 4; ++c) {
+          Eight<ARCHEAD_F16> e;
+          e.w[0] = bv[c][kc];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) acc[c] = mma<DT>(bv[c][kc], tv[k], acc[c]);
-      if constexpr (DT == ARCHEAD_F16) {
-        const float by = p.back[op * 16 + lr];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) sum[c] += acc[c] * by;
+          for (int i = 0; i < 8; ++i) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(e.at(i), t.at(i), acc[c], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);   // (one row's numbers at a time in registers: without it 231 us for 208 below)
+        }
       } else {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) sum[c] += acc[c];
+        for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] = mma<DT>(bv[c][kc], tv[k], acc[c]);
       }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sum[c] += DT == ARCHEAD_F16 ? acc[c] * by : acc[c];
     }
     if (lr >= g.len[ti]) continue;
     uint8_t* const out = p.out + at[u] * p.o_row;
