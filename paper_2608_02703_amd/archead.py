@@ -476,7 +476,6 @@ def rms_norm(x, weight, eps=1e-6, residual=None, offset=0.0, out=None, total=Non
     offset + weight (archead_rms_norm).  Returns the normed rows, and with a
     residual (normed rows, x + residual).  total (where the sum goes) and out may
     each be residual or x, but not both the same."""
-    import torch
     if out is None:
         out = x.new_empty(x.shape)
     total = _norm_call(x, weight, eps, residual, offset, total, out, None, None)
@@ -570,7 +569,8 @@ def head_loss(x, w, targets, loss=None, lse=None, ws=None):
     """Softmax cross entropy of the dense head w (bfloat16 [V, d]) on the hidden
     states x (bfloat16 [M, d]) without an [M, V] array of logits
     (archead_head_loss): returns (loss float32 [M], lse float32 [M]), both 0 where
-    targets (int32 or int64 [M]) lie outside [0, V)."""
+    targets (int32 or int64 [M]) lie outside [0, V).  The results carry no autograd
+    graph, also where x or w require gradients: head_loss_grad forms those."""
     import torch
     gpu, args, M, V, d, ws = _loss_call(x, w, targets, ws, 0)
     loss = torch.empty(M, dtype=torch.float32, device=x.device) if loss is None else loss

@@ -46,7 +46,9 @@ __device__ __forceinline__ int64_t target_of(const RowArgs& a, int64_t m) {
 // The live tokens (those with a target in the vocabulary) back to back, in their
 // order, with zeros behind each row up to whole stages and behind the last token's
 // for sums over tokens: tokens without a target cost no products, and nothing that
-// their rows hold can reach a sum.  Each workgroup counts the live tokens before its own.
+// their rows hold can reach a sum.  Each workgroup counts the live tokens before its own, in all
+// the targets (and g): one launch, the least for some thousand tokens (4096 x 64: 8 us in the loss, 11 in the
+// gradients), but the targets are read up to 1024 times (2^16 x 64: 95 and 160 us, 2^20 x 64: 2.1 and 3.2 ms).
 // g goes on in units of the largest, which the gradients get back in fp32: the entries of G
 // that weigh most, g (p - 1) at the targets, are then -1 + p for tokens that count alike, and
 // lose next to nothing in bf16 (g itself, say 1 / 87, would lose up to 2^-8 in each of them).

@@ -114,3 +114,19 @@ def test_infinite_factors(dtype, y):
     hit = torch.zeros_like(out, dtype=torch.bool)
     hit[i["ids"] == 1, 17] = True
     assert not torch.isfinite(out[hit]).any() and torch.equal(out[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("dtype,y", [("f16", "f32"), ("f16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("span", [6, 10, 13, 16, 20])
+@pytest.mark.parametrize("R", [16, 50])
+def test_ranks_within_a_span(R, span, dtype, y):
+    """Rows of a over 2^-6 to 2^-20, below and above where fp16's parts end, outputs of one rank alone."""
+    from paper_2608_02703_amd import adapters_add
+    M, N, K, n = 400, 3 * R, 256, 3
+    i = _inputs(M, N, K, R, n, dtype, y, seed=span)
+    i["y"].zero_()
+    i["a"] = (i["a"].double() * torch.exp2(-span * (torch.arange(R, device="cuda") * 7 % R) / (R - 1))[:, None]).to(i["a"].dtype)
+    at = torch.arange(N, device="cuda")
+    i["b"][:] = 0
+    i["b"][:, at, at % R] = (1 + at / N).to(i["b"].dtype)
+    _check(i, adapters_add(**i))
